@@ -279,6 +279,75 @@ int ssd_linear_bwd(int64_t rows, int32_t in_dim, int32_t out_dim, const void* x,
                    float* dw, uint32_t flags, void* hip_stream);
 
 /*
+ * Low-rank adapters of several requests at once beside a shared, frozen projection (ssd_linear's w): row t belongs to adapter
+ * a = row_adapter[t], or to none,
+ *     h[t,r]   = scale[a] sum_i x[t,i] a_a[r,i]                    out[t,o] = sum_i x[t,i] w[o,i] + sum_r h[t,r] b_a[o,r]
+ *     g[t,r]   = scale[a] sum_o dout[t,o] b_a[o,r]                 dx[t,i]  = sum_o dout[t,o] w[o,i] + sum_r g[t,r] a_a[r,i]
+ *     da_a[r,i] = sum over a's rows of g[t,r] x[t,i]               db_a[o,r] = sum over a's rows of dout[t,o] h[t,r]
+ * so that a batch may mix prompts and single tokens of requests with different adapters, and training several tasks.
+ * bf16 storage, fp32 accumulation; each of out and dx is rounded once.  A row meets its own adapter's values alone: infinities
+ * and NaN of another adapter or row do not reach it.  dw, where w is trained too, is ssd_linear_bwd's.
+ *   x, out, dout, dx and w as in ssd_linear_fwd / ssd_linear_bwd (column slices allowed; out_row_stride is dout's as well)
+ *   a [nadapters, rank, in_dim], b [nadapters, out_dim, rank] bf16, scale [nadapters] fp32, dense
+ *   hidden [rows, rank] fp32: h (zeros for rows without an adapter); written by the forward call if not NULL, and then taken by the
+ *          backward call, which works it out again if NULL.  Not read for dx alone.
+ *   da, db fp32, as a and b, overwritten (zeros for an adapter without rows) or added to under SSD_FLAG_ACCUM_PARAM (the only flag);
+ *          both or neither.  dx may be NULL too.  Sums run in a fixed order.
+ *   plan   what ssd_adapter_plan leaves for a batch: the rows in the order of their adapters.  It depends on row_adapter alone and
+ *          serves every projection of every layer, any number of calls, until the batch changes.  row_adapter [rows] int32 in any
+ *          order; whatever lies outside 0 .. nadapters - 1 means no adapter.  rows and nadapters of a call must be the plan's.
+ *   workspace: ssd_adapter_workspace_bytes bytes, 256-byte aligned (the forward call needs none where hidden is given)
+ * rank: a multiple of 8 up to 256 (pad smaller ones with zeros: their gradients stay zero).  in_dim, out_dim and strides: multiples
+ * of 8; pointers 16-byte aligned, the plan 256.  rows == 0: nothing but zeroed gradients.  Outputs must not overlap inputs or each
+ * other.  Everything is enqueued on hip_stream; nothing is allocated.
+ * Errors: SSD_ERR_NULL, SSD_ERR_SHAPE, SSD_ERR_DIVISIBILITY, SSD_ERR_ARG, SSD_ERR_WORKSPACE (workspace or plan), SSD_ERR_LAUNCH.
+ */
+#define SSD_MAX_ADAPTERS 16384
+#define SSD_MAX_ADAPTER_ROWS 1073741824
+typedef struct {
+    int64_t rows;
+    int32_t in_dim, out_dim, rank, nadapters;
+    int64_t x_row_stride, out_row_stride, dx_row_stride;  /* elements, 0 = dense; out_row_stride: of out and dout */
+} ssd_adapter_shape_t;
+size_t ssd_adapter_plan_bytes(int64_t rows, int32_t nadapters);   /* 0: invalid */
+int ssd_adapter_plan(int64_t rows, int32_t nadapters, const int32_t* row_adapter, void* plan, size_t plan_bytes, void* hip_stream);
+size_t ssd_adapter_workspace_bytes(const ssd_adapter_shape_t* shape, int32_t is_backward);   /* 0: invalid */
+int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const void* x, const void* w, const void* a, const void* b,
+                           const float* scale, const void* plan, void* out, float* hidden, void* workspace,
+                           size_t workspace_bytes, void* hip_stream);
+int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const void* x, const void* w, const void* a, const void* b,
+                           const float* scale, const void* plan, const void* dout, const float* hidden, void* dx, float* da,
+                           float* db, void* workspace, size_t workspace_bytes, uint32_t flags, void* hip_stream);
+
+/*
+ * The global norm of many gradients, and the gradients scaled down to it:
+ *     S = sum of g^2 over all tensors;   norm = sqrt(S);   out = g min(1, max_norm / (norm + 1e-6))
+ *   tensors: host array; grad and out are device pointers of numel elements each, fp32 or bf16 independently, aligned to their
+ *           elements.  out may be grad itself (same dtype), else nothing may overlap.  Any number of tensors, any numel >= 0.
+ *   plan    device memory of ssd_grad_plan_bytes bytes, 256-byte aligned, which ssd_grad_plan fills for these pointers and which
+ *           serves any number of calls; *pieces (host) is what the other two calls take.  Calls that share a plan must not overlap
+ *           in time (it holds their partial sums).
+ *   ssd_grad_norm: sum_sq (one double, device) = S, in fp64, in a fixed order.  Gradients that lie on several devices: add up their S
+ *           in front of ssd_grad_clip.
+ *   ssd_grad_clip: scales by the factor of *sum_sq; norm (one float, device) = sqrt(S), or NULL.  A gradient that is its own result is
+ *           left alone where the factor is 1.  Non-finite gradients act as the formula says: an infinite norm gives a factor of 0
+ *           (and NaN where 0 meets an infinity), a NaN makes everything NaN; the norm tells a caller to drop the step.
+ * max_norm >= 0, infinity for the norm alone.  Everything is enqueued on hip_stream, nothing is allocated, the host does not wait.
+ * Errors: SSD_ERR_NULL, SSD_ERR_SHAPE, SSD_ERR_DTYPE, SSD_ERR_ARG, SSD_ERR_WORKSPACE, SSD_ERR_LAUNCH.
+ */
+typedef struct {
+    const void* grad;
+    void* out;
+    int64_t numel;
+    int32_t grad_dtype, out_dtype;   /* ssd_dtype_t */
+} ssd_grad_tensor_t;
+size_t ssd_grad_plan_bytes(int32_t ntensors, const ssd_grad_tensor_t* tensors /*host*/);   /* 0: invalid */
+int ssd_grad_plan(int32_t ntensors, const ssd_grad_tensor_t* tensors /*host*/, void* plan, size_t plan_bytes, int64_t* pieces /*host*/,
+                  void* hip_stream);
+int ssd_grad_norm(void* plan, int64_t pieces, double* sum_sq, void* hip_stream);
+int ssd_grad_clip(void* plan, int64_t pieces, const double* sum_sq, float max_norm, float* norm, void* hip_stream);
+
+/*
  * Backward (Recompute_Forward + Backward of Alg. 2 over every segment, right to left).
  * Gradients of  <dy, y> + <dfinal_state, final_state>.
  *   inputs as in ssd_fwd, plus

@@ -21,6 +21,8 @@ EXPORTS = ("ssd_workspace_bytes", "ssd_workspace_bytes_flags", "ssd_fwd", "ssd_b
            "ssd_init", "ssd_fwd_static_bytes", "ssd_fwd_static",
            "ssd_conv1d_workspace_bytes", "ssd_conv1d_fwd", "ssd_conv1d_bwd",
            "ssd_gated_norm_workspace_bytes", "ssd_gated_norm_fwd", "ssd_gated_norm_bwd", "ssd_linear_fwd", "ssd_linear_bwd",
+           "ssd_adapter_plan_bytes", "ssd_adapter_plan", "ssd_adapter_workspace_bytes", "ssd_adapter_linear_fwd", "ssd_adapter_linear_bwd",
+           "ssd_grad_plan_bytes", "ssd_grad_plan", "ssd_grad_norm", "ssd_grad_clip",
            "magc_block_workspace_bytes", "magc_block_fwd", "magc_block_bwd",
            "magc_blockstack_workspace_bytes", "magc_blockstack_pass_bytes", "magc_blockstack_fwd", "magc_blockstack_bwd", "magc_blockstack_infer", "magc_blockstack_decode",
            "magc_stack_workspace_bytes", "magc_stack_fwd",
@@ -43,6 +45,17 @@ class ssd_conv_shape_t(ctypes.Structure):
 class ssd_norm_shape_t(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("ngroups", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("rows", ctypes.c_int64), ("y_row_stride", ctypes.c_int64), ("z_row_stride", ctypes.c_int64)]
+
+
+class ssd_adapter_shape_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_dim", ctypes.c_int32), ("out_dim", ctypes.c_int32), ("rank", ctypes.c_int32),
+                ("nadapters", ctypes.c_int32), ("x_row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64),
+                ("dx_row_stride", ctypes.c_int64)]
+
+
+class ssd_grad_tensor_t(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64), ("grad_dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32)]
 
 
 class magc_block_shape_t(ctypes.Structure):
@@ -130,6 +143,25 @@ def lib():
         L.ssd_linear_fwd.argtypes = [i64, i32, i32, vp, i64, vp, vp, i64, vp]
         L.ssd_linear_bwd.restype = ctypes.c_int
         L.ssd_linear_bwd.argtypes = [i64, i32, i32, vp, i64, vp, vp, i64, vp, i64, vp, u32, vp]
+        ashp, gten = ctypes.POINTER(ssd_adapter_shape_t), ctypes.POINTER(ssd_grad_tensor_t)
+        L.ssd_adapter_plan_bytes.restype = sz
+        L.ssd_adapter_plan_bytes.argtypes = [i64, i32]
+        L.ssd_adapter_plan.restype = ctypes.c_int
+        L.ssd_adapter_plan.argtypes = [i64, i32, vp, vp, sz, vp]
+        L.ssd_adapter_workspace_bytes.restype = sz
+        L.ssd_adapter_workspace_bytes.argtypes = [ashp, i32]
+        L.ssd_adapter_linear_fwd.restype = ctypes.c_int
+        L.ssd_adapter_linear_fwd.argtypes = [ashp] + [vp] * 9 + [sz, vp]
+        L.ssd_adapter_linear_bwd.restype = ctypes.c_int
+        L.ssd_adapter_linear_bwd.argtypes = [ashp] + [vp] * 12 + [sz, u32, vp]
+        L.ssd_grad_plan_bytes.restype = sz
+        L.ssd_grad_plan_bytes.argtypes = [i32, gten]
+        L.ssd_grad_plan.restype = ctypes.c_int
+        L.ssd_grad_plan.argtypes = [i32, gten, vp, sz, ctypes.POINTER(i64), vp]
+        L.ssd_grad_norm.restype = ctypes.c_int
+        L.ssd_grad_norm.argtypes = [vp, i64, vp, vp]
+        L.ssd_grad_clip.restype = ctypes.c_int
+        L.ssd_grad_clip.argtypes = [vp, i64, vp, ctypes.c_float, vp, vp]
         bshp, bpar, bgr = (ctypes.POINTER(t) for t in (magc_block_shape_t, magc_block_params_t, magc_block_grads_t))
         L.magc_block_workspace_bytes.restype = sz
         L.magc_block_workspace_bytes.argtypes = [bshp, i32]
@@ -513,6 +545,177 @@ def ssd_linear_bwd(x, w, dout, want_dx=True, want_dw=True, flags=0, dx=None, dw=
     if rc != 0:
         raise SSDError(rc, "ssd_linear_bwd")
     return {"dx": dx, "dw": dw}
+
+
+class AdapterPlan:
+    """The rows of a batch in the order of their adapters (ssd_adapter_plan): serves every projection until the batch changes."""
+
+    def __init__(self, buffer, rows: int, nadapters: int):
+        self.buffer, self.rows, self.nadapters = buffer, rows, nadapters
+
+
+def ssd_adapter_plan(row_adapter, nadapters: int) -> AdapterPlan:
+    """Plan of a batch whose row t takes adapter row_adapter[t] (int32 [rows] on the device; outside 0 .. nadapters - 1: none)."""
+    import torch
+    if row_adapter.dim() != 1 or not row_adapter.is_cuda or row_adapter.dtype != torch.int32 or not row_adapter.is_contiguous():
+        raise ValueError("row_adapter must be a dense [rows] int32 device tensor")
+    rows = row_adapter.shape[0]
+    nbytes = int(lib().ssd_adapter_plan_bytes(rows, nadapters))
+    buf = _workspace(nbytes, row_adapter.device)
+    rc = lib().ssd_adapter_plan(rows, nadapters, _ptr(row_adapter), _ptr(buf), nbytes, _stream(row_adapter))
+    if rc != 0:
+        raise SSDError(rc, "ssd_adapter_plan")
+    return AdapterPlan(buf, rows, nadapters)
+
+
+def _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, strides, *same_device) -> ssd_adapter_shape_t:
+    import torch
+    if not isinstance(plan, AdapterPlan):
+        raise ValueError("plan must be ssd_adapter_plan's")
+    rows = plan.rows
+    if a.dim() != 3 or b.dim() != 3 or a.dtype != torch.bfloat16 or b.dtype != torch.bfloat16 or not a.is_contiguous() or not b.is_contiguous():
+        raise ValueError("a and b must be dense bf16 [nadapters, rank, in_dim] and [nadapters, out_dim, rank]")
+    n, rank, _ = a.shape
+    if a.shape != (n, rank, in_dim) or b.shape != (n, out_dim, rank):
+        raise ValueError(f"a must be [nadapters, rank, {in_dim}] and b [nadapters, {out_dim}, rank], got {tuple(a.shape)} and {tuple(b.shape)}")
+    if scale.dtype != torch.float32 or scale.shape != (n,) or not scale.is_contiguous():
+        raise ValueError("scale must be a dense fp32 [nadapters] device tensor")
+    if plan.nadapters != n:
+        raise ValueError(f"the plan is of {plan.nadapters} adapters, a and b have {n}")
+    if w is not None and (w.dtype != torch.bfloat16 or w.shape != (out_dim, in_dim) or not w.is_contiguous()):
+        raise ValueError("w must be a dense [out_dim, in_dim] bf16 device tensor")
+    for t in (a, b, scale, plan.buffer, w, *same_device):
+        if t is not None and t.device != x.device:
+            raise ValueError(f"all tensors must be on {x.device}, got {t.device}")
+    return ssd_adapter_shape_t(rows, in_dim, out_dim, rank, n, *strides)
+
+
+def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False, hidden=None, workspace=None):
+    """dict(out, hidden): out [rows, out_dim] = x @ w^T + h @ b_a^T with h = scale_a x @ a_a^T for the adapter a of each row (`plan`:
+    ssd_adapter_plan's).  a [nadapters, rank, in_dim], b [nadapters, out_dim, rank], scale [nadapters] fp32.  `hidden` is h, fp32
+    [rows, rank], kept for ssd_adapter_linear_bwd where want_hidden is set or the tensor given, else None."""
+    import torch
+    ldx = _rows_view(x, "x")
+    rows, in_dim = x.shape
+    out_dim = w.shape[0]
+    if out is None:
+        out = torch.empty((rows, out_dim), dtype=torch.bfloat16, device=x.device)
+    ldo = _rows_view(out, "out")
+    shape = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldo, 0), out, hidden)
+    if rows != plan.rows or out.shape != (rows, out_dim):
+        raise ValueError(f"x and out must have the plan's {plan.rows} rows and w's {out_dim} columns")
+    if hidden is None and want_hidden:
+        hidden = torch.empty((rows, shape.rank), dtype=torch.float32, device=x.device)
+    if hidden is not None:
+        _check_hidden(hidden, rows, shape.rank)
+    elif workspace is None:
+        workspace = _workspace(int(lib().ssd_adapter_workspace_bytes(ctypes.byref(shape), 0)), x.device)
+    rc = lib().ssd_adapter_linear_fwd(ctypes.byref(shape), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(out),
+                                      _ptr(hidden), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(x))
+    if rc != 0:
+        raise SSDError(rc, "ssd_adapter_linear_fwd")
+    return {"out": out, "hidden": hidden}
+
+
+def _check_hidden(hidden, rows, rank):
+    import torch
+    if hidden.dtype != torch.float32 or hidden.shape != (rows, rank) or not hidden.is_contiguous():
+        raise ValueError("hidden must be a dense fp32 [rows, rank] device tensor")
+
+
+def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=True, want_dab=True, flags=0, dx=None, da=None, db=None,
+                           workspace=None):
+    """dict(dx, da, db) for the loss <dout, out>; da and db are fp32, shaped as a and b; w is frozen (its gradient is ssd_linear_bwd's).
+    `hidden`: the forward call's, worked out again if None."""
+    import torch
+    ldx, ldd = _rows_view(x, "x"), _rows_view(dout, "dout")
+    rows, in_dim = x.shape
+    out_dim = dout.shape[1]
+    if dx is None and want_dx:
+        dx = torch.empty((rows, in_dim), dtype=torch.bfloat16, device=x.device)
+    lddx = _rows_view(dx, "dx") if dx is not None else 0
+    shape = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldd, lddx), dout, dx, da, db, hidden)
+    if rows != plan.rows or dout.shape[0] != rows or (dx is not None and dx.shape != x.shape):
+        raise ValueError(f"x, dout and dx must have the plan's {plan.rows} rows, dx as many columns as x")
+    if (da is None) != (db is None):
+        raise ValueError("da and db: both or neither")
+    if da is None and want_dab:
+        da, db = (torch.empty(t.shape, dtype=torch.float32, device=x.device) for t in (a, b))
+    for name, t, like in (("da", da, a), ("db", db, b)):
+        if t is not None and (t.dtype != torch.float32 or t.shape != like.shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a dense fp32 {tuple(like.shape)} device tensor")
+    if hidden is not None:
+        _check_hidden(hidden, rows, shape.rank)
+    if workspace is None:
+        workspace = _workspace(int(lib().ssd_adapter_workspace_bytes(ctypes.byref(shape), 1)), x.device)
+    rc = lib().ssd_adapter_linear_bwd(ctypes.byref(shape), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(dout),
+                                      _ptr(hidden), _ptr(dx), _ptr(da), _ptr(db), _ptr(workspace), workspace.numel(), flags, _stream(x))
+    if rc != 0:
+        raise SSDError(rc, "ssd_adapter_linear_bwd")
+    return {"dx": dx, "da": da, "db": db}
+
+
+class GradPlan:
+    """The pieces of a list of gradients (ssd_grad_plan).  It keeps the tensors alive whose addresses it holds."""
+
+    def __init__(self, buffer, pieces: int, grads, outs):
+        self.buffer, self.pieces, self.grads, self.outs = buffer, pieces, grads, outs
+
+
+def ssd_grad_plan(grads, outs=None) -> GradPlan:
+    """Plan for clipping `grads` (dense fp32 or bf16 device tensors, at least one) into `outs` (same shapes, fp32 or bf16; None: in place)."""
+    import torch
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    if not grads or len(outs) != len(grads):
+        raise ValueError("one result for each gradient, at least one")
+    dev, kinds = grads[0].device, {torch.float32: SSD_F32, torch.bfloat16: SSD_BF16}
+    arr = (ssd_grad_tensor_t * len(grads))()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        for t in (g, o):
+            if not t.is_cuda or t.device != dev or t.dtype not in kinds or not t.is_contiguous() or t.shape != g.shape:
+                raise ValueError("gradients and results must be dense fp32 or bf16 tensors of the same shapes on one device")
+        arr[i] = ssd_grad_tensor_t(_ptr(g), _ptr(o), g.numel(), kinds[g.dtype], kinds[o.dtype])
+    nbytes = int(lib().ssd_grad_plan_bytes(len(grads), arr))
+    buf, pieces = _workspace(nbytes, dev), ctypes.c_int64()
+    rc = lib().ssd_grad_plan(len(grads), arr, _ptr(buf), buf.numel(), ctypes.byref(pieces), _stream(buf))
+    if rc != 0:
+        raise SSDError(rc, "ssd_grad_plan")
+    return GradPlan(buf, pieces.value, grads, outs)
+
+
+def ssd_grad_norm(plan: GradPlan, sum_sq=None):
+    """sum_sq [1] fp64: the sum of squares of all of the plan's gradients (on several devices: add them up before ssd_grad_clip)."""
+    import torch
+    if sum_sq is None:
+        sum_sq = torch.empty(1, dtype=torch.float64, device=plan.buffer.device)
+    _check_sum_sq(sum_sq, plan)
+    rc = lib().ssd_grad_norm(_ptr(plan.buffer), plan.pieces, _ptr(sum_sq), _stream(plan.buffer))
+    if rc != 0:
+        raise SSDError(rc, "ssd_grad_norm")
+    return sum_sq
+
+
+def _check_sum_sq(sum_sq, plan):
+    import torch
+    if sum_sq.dtype != torch.float64 or sum_sq.numel() != 1 or sum_sq.device != plan.buffer.device:
+        raise ValueError("sum_sq must be one fp64 value on the plan's device")
+
+
+def ssd_grad_clip(plan: GradPlan, max_norm: float, sum_sq=None):
+    """Scales the plan's gradients by min(1, max_norm / (norm + 1e-6)) into its results and returns norm [1] fp32.  sum_sq: the sum of
+    squares that the norm is the root of (None: the plan's own, by ssd_grad_norm)."""
+    import torch
+    if not max_norm >= 0:
+        raise ValueError("max_norm must not be negative")
+    if sum_sq is None:
+        sum_sq = ssd_grad_norm(plan)
+    _check_sum_sq(sum_sq, plan)
+    norm = torch.empty(1, dtype=torch.float32, device=plan.buffer.device)
+    rc = lib().ssd_grad_clip(_ptr(plan.buffer), plan.pieces, _ptr(sum_sq), max_norm, _ptr(norm), _stream(plan.buffer))
+    if rc != 0:
+        raise SSDError(rc, "ssd_grad_clip")
+    return norm
 
 
 def _block_layout(u, params, nheads, headdim, ngroups, dstate, chunk, segment, eps):

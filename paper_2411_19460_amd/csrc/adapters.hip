@@ -1,0 +1,575 @@
+// Low-rank adapters beside a shared projection: every row t of a call belongs to a request that has an adapter a(t), or none,
+//     h[t, :] = s_a x[t, :] A_a^T            out[t, :] = x[t, :] W^T + h[t, :] B_a^T
+//     g[t, :] = s_a dout[t, :] B_a           dx[t, :]  = dout[t, :] W + g[t, :] A_a
+//     dA_a = sum_{t of a} g[t, :]^T x[t, :]  dB_a = sum_{t of a} dout[t, :]^T h[t, :]
+// with the projection W frozen.  The products with W and the low-rank terms that join them are tiles of linear.hip; here are the plan
+// of a batch (which rows share an adapter), the narrow products h and g, and the adapters' gradients.
+// h and g are fp32, and so is everything that is summed: the gradients leave in fp32, and would lose 16 of its bits with either in bf16.
+#include <string.h>
+
+#include "mfma_common.h"
+
+namespace ssdk {
+namespace {
+
+using namespace mf;
+
+// ---- the plan of a batch ----
+// Rows in the order of their adapters (stable; rows without one last), cut into units of rows that share one: short units for the
+// narrow products, long ones for the gradients, where a unit is what is summed before anything leaves for memory.  And for every tile
+// of the wide product the adapters that its rows have.  Words of 32 bits; host and device derive the places from (rows, adapters).
+constexpr int SHORT_UNIT = 32, PLAN_HDR = 16, MAX_RANK = 256;
+
+struct Plan {
+    int rows, n, long_unit, max_short, max_long, tiles;
+    int64_t ids, perm, start, first_short, first_long, first_slot, short_a, long_a, tile_n, tile_a, counts, words;
+};
+
+int long_unit_of(int64_t rows) {  // about sixteen units where all rows share an adapter
+    const int64_t u = (rows / 16 + 63) / 64 * 64;
+    return (int)(u < 512 ? 512 : u);
+}
+
+Plan plan_of(int64_t rows, int32_t n) {
+    Plan p;
+    p.rows = (int)rows;
+    p.n = n;
+    p.long_unit = long_unit_of(rows);
+    auto least = [](int64_t a, int64_t b) { return (int)(a < b ? a : b); };
+    p.max_short = least(rows, rows / SHORT_UNIT + n + 1);
+    p.max_long = least(rows, rows / p.long_unit + n);
+    p.tiles = (int)((rows + LOW_TILE - 1) / LOW_TILE);
+    int64_t at = PLAN_HDR;
+    auto take = [&](int64_t words) {
+        const int64_t here = at;
+        at += (words + 3) / 4 * 4;
+        return here;
+    };
+    p.ids = take(rows);
+    p.perm = take(rows);
+    p.start = take(n + 2);        // of adapter a in perm; [n]: of the rows without one
+    p.first_short = take(n + 2);
+    p.first_long = take(n + 1);
+    p.first_slot = take(n + 1);   // partial sums of the gradients: adapters of several long units
+    p.short_a = take(p.max_short);
+    p.long_a = take(p.max_long);
+    p.tile_n = take(p.tiles);
+    p.tile_a = take((int64_t)p.tiles * LOW_TILE);
+    p.counts = take(n + 1);
+    p.words = at;
+    return p;
+}
+// Adapters of several long units have at most two units for each long_unit of their rows.
+int64_t most_slots(const Plan& p) {
+    const int64_t s = 2 * ((int64_t)p.rows / p.long_unit);
+    return s < p.max_long ? s : p.max_long;
+}
+
+constexpr int PTHR = 256;
+
+__device__ __forceinline__ int block_sum(int v, int* lds) {  // every thread gets the sum over the workgroup
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+__device__ __forceinline__ int clean(int a, int n) { return a >= 0 && a < n ? a : -1; }
+
+// Workgroups 0 .. tiles - 1: the rows' adapters (anything outside 0 .. n - 1 is none) and the list of a tile; the others count the rows
+// of an adapter each (the last: of none).
+__global__ __launch_bounds__(PTHR) void k_plan_count(Plan p, const int* row_adapter, int* plan) {
+    __shared__ int lds[LOW_TILE];
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x < p.tiles) {
+        const int64_t row = (int64_t)blockIdx.x * LOW_TILE + tid;
+        const int a = row < p.rows ? clean(row_adapter[row], p.n) : -2;
+        if (row < p.rows) plan[p.ids + row] = a;
+        lds[tid] = a;
+        __syncthreads();
+        bool first = a >= 0;
+        for (int j = 0; j < tid; ++j) first = first && lds[j] != a;
+        const int whole = __syncthreads_and(a == -2 || a == lds[0]);
+        lds[tid] = first ? a : 0x7fffffff;
+        __syncthreads();
+        int place = 0;
+        for (int j = 0; j < LOW_TILE; ++j) place += lds[j] < a;
+        if (first) plan[p.tile_a + (int64_t)blockIdx.x * LOW_TILE + place] = a;
+        const int listed = block_sum(first, lds);
+        if (tid == 0) plan[p.tile_n + blockIdx.x] = listed | (whole && listed == 1 ? 0x10000 : 0);
+        return;
+    }
+    const int mine = blockIdx.x - p.tiles;
+    int c = 0;
+    for (int64_t r = tid; r < p.rows; r += PTHR) {
+        const int a = clean(row_adapter[r], p.n);
+        c += (a < 0 ? p.n : a) == mine;
+    }
+    c = block_sum(c, lds);
+    if (tid == 0) plan[p.counts + mine] = c;
+}
+
+// Workgroup a: where the rows and units of adapter a begin, its rows in order, its units.
+__global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
+    __shared__ int lds[4];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, a = blockIdx.x;
+    auto shorts = [](int c) { return (c + SHORT_UNIT - 1) / SHORT_UNIT; };
+    auto longs = [&](int c) { return (c + p.long_unit - 1) / p.long_unit; };
+    int start = 0, fs = 0, fl = 0, fp = 0;
+    for (int b = tid; b < a; b += PTHR) {
+        const int c = plan[p.counts + b], l = longs(c);
+        start += c;
+        fs += shorts(c);
+        fl += l;
+        fp += l > 1 ? l : 0;
+    }
+    start = block_sum(start, lds);
+    fs = block_sum(fs, lds);
+    fl = block_sum(fl, lds);
+    fp = block_sum(fp, lds);
+    const int mine = plan[p.counts + a], ns = shorts(mine), nl = longs(mine);
+    if (tid == 0) {
+        plan[p.start + a] = start;
+        plan[p.first_short + a] = fs;
+        if (a < p.n) {
+            plan[p.first_long + a] = fl;
+            plan[p.first_slot + a] = fp;
+        } else {
+            plan[p.start + a + 1] = start + mine;
+            plan[p.first_short + a + 1] = fs + ns;
+            plan[p.first_long + a] = fl;
+            plan[p.first_slot + a] = fp;
+            plan[0] = fs + ns;
+            plan[1] = fl;
+        }
+    }
+    for (int u = tid; u < ns; u += PTHR) plan[p.short_a + fs + u] = a;
+    if (a < p.n)
+        for (int u = tid; u < nl; u += PTHR) plan[p.long_a + fl + u] = a;
+    int at = start;
+    const int wanted = a < p.n ? a : -1;
+    for (int64_t r0 = 0; r0 < p.rows && at < start + mine; r0 += PTHR) {
+        const int64_t r = r0 + tid;
+        const bool is = r < p.rows && plan[p.ids + r] == wanted;
+        const uint64_t m = __ballot(is);
+        __syncthreads();
+        if (lane == 0) lds[wv] = __popcll(m);
+        __syncthreads();
+        int before = 0;
+        for (int q = 0; q < 4; ++q) before += q < wv ? lds[q] : 0;
+        if (is) plan[p.perm + at + before + __popcll(m & ((1ull << lane) - 1))] = (int)r;
+        at += lds[0] + lds[1] + lds[2] + lds[3];
+    }
+}
+
+// ---- the narrow products ----
+// low[t, r] = s_a sum_k X[t, k] U_a[r, k].  A workgroup takes a short unit and 16 RT of the ranks; its eight waves share out k in steps
+// of 64, of which a quarter wave takes sixteen consecutive k (32 bytes of a row at a lane), and their sums meet in LDS.  KROW: U is
+// stored with k as the row index ([K, rank], the output side of an adapter) and goes through LDS to be read transposed.
+struct LowParams {
+    const __bf16* x;
+    int64_t ldx;
+    const __bf16* u;
+    const float* scale;
+    float* low;
+    int K, rank;
+};
+constexpr int LWAVES = 8;
+
+template <int RT>
+constexpr int low_pitch() { return 32 * RT + 16; }
+template <int RT, bool KROW>
+constexpr int low_lds() {
+    constexpr int tiles = KROW ? LWAVES * 64 * low_pitch<RT>() : 0, sums = LWAVES * SHORT_UNIT * 16 * RT * 4;
+    return tiles > sums ? tiles : sums;
+}
+
+template <int RT, bool KROW, int MT>
+__device__ __forceinline__ void low_unit(const LowParams& lp, const int* rows, int cnt, int a, int r0, char* lds) {
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
+    const int nr = lp.rank - r0 < 16 * RT ? lp.rank - r0 : 16 * RT;  // ranks of this workgroup
+    const __bf16* xr[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int r = i * 16 + l16;
+        xr[i] = lp.x + rows[r < cnt ? r : cnt - 1] * lp.ldx;
+    }
+    const __bf16* ua = lp.u + (int64_t)a * lp.rank * lp.K;
+    const __bf16* ur[RT];  // KROW: not used
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int r = r0 + 16 * t + l16;
+        ur[t] = ua + (int64_t)(r < lp.rank ? r : lp.rank - 1) * lp.K;
+    }
+    char* mine = lds + w * 64 * low_pitch<RT>();
+    const int vpr = nr / 8;  // KROW: 16-byte pieces of a row of U
+    f32x4 acc[RT][MT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[t][i] = (f32x4)(0.f);
+    for (int k0 = 64 * w; k0 < lp.K; k0 += 64 * LWAVES) {
+        bf16x8 xv[MT][2], uv[RT][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = k0 + 16 * q + 8 * h;
+            const bool in = k < lp.K;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                xv[i][h] = (bf16x8)((__bf16)0.f);
+                if (in) xv[i][h] = *(const bf16x8*)(xr[i] + k);
+            }
+            if (!KROW)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    uv[t][h] = (bf16x8)((__bf16)0.f);
+                    if (in) uv[t][h] = *(const bf16x8*)(ur[t] + k);
+                }
+        }
+        if (KROW) {
+            // the wave's own rows: LDS operations of a wave are done in order
+#pragma unroll
+            for (int i = 0; i < 2 * RT; ++i) {
+                const int v = i * 64 + lane, k = v / vpr, c = v - k * vpr;
+                bf16x8 b = (bf16x8)((__bf16)0.f);
+                if (k < 64 && k0 + k < lp.K) b = *(const bf16x8*)(ua + (int64_t)(k0 + k) * lp.rank + r0 + 8 * c);
+                if (k < 64) *(bf16x8*)(mine + k * low_pitch<RT>() + 16 * c) = b;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const char* p = mine + (16 * q + 8 * h + (l16 >> 2)) * low_pitch<RT>() + 32 * t + 8 * (l16 & 3);
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * low_pitch<RT>()));
+                    uv[t][h] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uv[t][h], xv[i][h], acc[t][i], 0, 0, 0);
+    }
+    __syncthreads();
+    // lane -> row l16 of the unit's tile i, four consecutive ranks
+    float* sums = (float*)lds;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) *(f32x4*)(sums + (w * SHORT_UNIT + i * 16 + l16) * 16 * RT + 16 * t + 4 * q) = acc[t][i];
+    __syncthreads();
+    const float s = lp.scale[a];
+    for (int v = tid; v < MT * 16 * 4 * RT; v += 64 * LWAVES) {
+        const int row = v / (4 * RT), c = 4 * (v - row * 4 * RT);
+        if (row >= cnt || c >= nr) continue;
+        f32x4 o = (f32x4)(0.f);
+#pragma unroll
+        for (int u = 0; u < LWAVES; ++u) o += *(const f32x4*)(sums + (u * SHORT_UNIT + row) * 16 * RT + c);
+        *(f32x4*)(lp.low + (int64_t)rows[row] * lp.rank + r0 + c) = o * s;
+    }
+}
+
+template <int RT, bool KROW>
+__global__ __launch_bounds__(64 * LWAVES) void k_low(LowParams lp, Plan p, const int* plan) {
+    extern __shared__ __attribute__((aligned(16))) char low_lds_mem[];
+    const int u = blockIdx.x;
+    if (u >= plan[0]) return;
+    const int a = plan[p.short_a + u], first = plan[p.start + a] + SHORT_UNIT * (u - plan[p.first_short + a]);
+    const int left = plan[p.start + a + 1] - first, cnt = left < SHORT_UNIT ? left : SHORT_UNIT, r0 = blockIdx.y * 16 * RT;
+    const int* rows = plan + p.perm + first;
+    if (a == p.n) {  // rows without an adapter
+        const int nr = lp.rank - r0 < 16 * RT ? lp.rank - r0 : 16 * RT;
+        for (int v = threadIdx.x; v < cnt * nr; v += 64 * LWAVES) lp.low[(int64_t)rows[v / nr] * lp.rank + r0 + v % nr] = 0.f;
+        return;
+    }
+    if (cnt <= 16) low_unit<RT, KROW, 1>(lp, rows, cnt, a, r0, low_lds_mem);
+    else low_unit<RT, KROW, 2>(lp, rows, cnt, a, r0, low_lds_mem);
+}
+
+template <int RT, bool KROW>
+hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, hipStream_t st) {
+    constexpr int LDS = low_lds<RT, KROW>();
+    static bool raised[64];
+    if (LDS > 65536) {
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+        if (!raised[dev]) {
+            const hipError_t e = hipFuncSetAttribute((const void*)k_low<RT, KROW>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+            if (e != hipSuccess) return e;
+            raised[dev] = true;
+        }
+    }
+    hipLaunchKernelGGL((k_low<RT, KROW>), dim3(p.max_short, (lp.rank + 16 * RT - 1) / (16 * RT)), dim3(64 * LWAVES), LDS, st, lp, p, plan);
+    return hipGetLastError();
+}
+
+template <bool KROW>
+hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* plan, hipStream_t st) {
+    if (lp.rank <= 16) return launch_low_rt<1, KROW>(lp, p, plan, st);
+    if (lp.rank <= 32) return launch_low_rt<2, KROW>(lp, p, plan, st);
+    return launch_low_rt<4, KROW>(lp, p, plan, st);
+}
+
+// ---- the adapters' gradients ----
+// G[r, c] = sum over the rows t of a long unit of S[t, r] X[t, c], X = x (dA, with S = g) or dout (dB, with S = h).  The contraction runs
+// over the rows of both operands, which therefore go through LDS to be read transposed.  S is fp32: three bf16 parts hold its 24 bits,
+// and each takes an MFMA (the arithmetic stays far below the reading of X).  A workgroup takes 128 columns and up to 64 ranks of a unit.
+// Rows beyond the unit's end are zero in both operands.
+struct GradJob {
+    const __bf16* x;
+    int64_t ldx;
+    const float* s;
+    float* out;   // [adapters][rank][cols], or transposed [adapters][cols][rank]
+    float* part;  // the same, by slots
+    int cols;
+    int blocks;   // of columns
+};
+struct GradParams {
+    GradJob job[2];  // 0: dA, 1: dB (transposed)
+    int rank, accumulate;
+};
+constexpr int GCOLS = 128, GRANKS = 64, GXP = GCOLS * 2 + 16, GSP = GRANKS * 2 + 16;
+
+template <int RT, bool TRANS>
+__device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& gp, const Plan& p, const int* plan, int u, int cb, int r0, char* lds) {
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
+    const int a = plan[p.long_a + u], fl = plan[p.first_long + a], nl = plan[p.first_long + a + 1] - fl;
+    const int first = plan[p.start + a] + p.long_unit * (u - fl), left = plan[p.start + a + 1] - first, cnt = left < p.long_unit ? left : p.long_unit;
+    const int* rows = plan + p.perm + first;
+    const int c0 = cb * GCOLS;
+    char *lx = lds, *ls = lds + 64 * GXP;
+    f32x4 acc[RT][2];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[t][j] = (f32x4)(0.f);
+    for (int t0 = 0; t0 < cnt; t0 += 64) {
+        bf16x8 xv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // 64 rows of 16 pieces
+            const int v = i * 256 + tid, t = v >> 4, c = (v & 15) * 8;
+            xv[i] = (bf16x8)((__bf16)0.f);
+            if (t0 + t < cnt && c0 + c < jb.cols) xv[i] = *(const bf16x8*)(jb.x + rows[t0 + t] * jb.ldx + c0 + c);
+        }
+        f32x4 sv[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {  // 64 rows of 4 RT pieces of four ranks
+            const int v = i * 256 + tid, t = v / (4 * RT), r = 4 * (v % (4 * RT));
+            sv[i] = (f32x4)(0.f);
+            if (t0 + t < cnt && r0 + r < gp.rank) sv[i] = *(const f32x4*)(jb.s + (int64_t)rows[t0 + t] * gp.rank + r0 + r);
+        }
+        __syncthreads();  // the operands before these have been read
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int v = i * 256 + tid;
+            *(bf16x8*)(lx + (v >> 4) * GXP + (v & 15) * 16) = xv[i];
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int v = i * 256 + tid, t = v / (4 * RT), r = 4 * (v % (4 * RT));
+#pragma unroll
+            for (int part = 0; part < 3; ++part) {
+                const bf16x4 b = __builtin_convertvector(sv[i], bf16x4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sv[i][e] = __builtin_isinf((float)b[e]) ? 0.f : sv[i][e] - (float)b[e];  // (an infinity: the first part alone)
+                *(bf16x4*)(ls + (part * 64 + t) * GSP + 2 * r) = b;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = 32 * h + 8 * q + (l16 >> 2);
+            bf16x8 xo[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const char* at = lx + k * GXP + (w * 32 + j * 16) * 2 + 8 * (l16 & 3);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * GXP));
+                xo[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+#pragma unroll
+            for (int part = 0; part < 3; ++part)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const char* at = ls + (part * 64 + k) * GSP + 32 * t + 8 * (l16 & 3);
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * GSP));
+                    const bf16x8 so = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[t][j] = TRANS ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(so, xo[j], acc[t][j], 0, 0, 0)
+                                          : __builtin_amdgcn_mfma_f32_16x16x32_bf16(xo[j], so, acc[t][j], 0, 0, 0);
+                }
+        }
+    }
+    // TRANS: lane -> column l16, four consecutive ranks; else lane -> rank l16, four consecutive columns
+    const bool direct = nl == 1;
+    const int64_t size = (int64_t)gp.rank * jb.cols;
+    float* org = direct ? jb.out + a * size : jb.part + (plan[p.first_slot + a] + (u - fl)) * size;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = r0 + 16 * t + (TRANS ? 4 * q : l16), c = c0 + w * 32 + j * 16 + (TRANS ? l16 : 4 * q);
+            if (r >= gp.rank || c >= jb.cols) continue;
+            f32x4* at = (f32x4*)(org + (TRANS ? (int64_t)c * gp.rank + r : (int64_t)r * jb.cols + c));
+            *at = direct && gp.accumulate ? *at + acc[t][j] : acc[t][j];
+        }
+}
+
+template <int RT>
+__global__ __launch_bounds__(256) void k_adapter_grads(GradParams gp, Plan p, const int* plan) {
+    __shared__ __attribute__((aligned(16))) char lds[64 * GXP + 3 * 64 * GSP];
+    const int u = blockIdx.y;
+    if (u >= plan[1]) return;
+    const int b = blockIdx.x, r0 = blockIdx.z * 16 * RT;
+    if (b < gp.job[0].blocks) grad_unit<RT, false>(gp.job[0], gp, p, plan, u, b, r0, lds);
+    else grad_unit<RT, true>(gp.job[1], gp, p, plan, u, b - gp.job[0].blocks, r0, lds);
+}
+
+// Adapters of several units: their sums in order; adapters without a row: zeros.
+__global__ __launch_bounds__(256) void k_adapter_grads_sum(GradParams gp, Plan p, const int* plan, int blocks0) {
+    const int a = blockIdx.y;
+    const int nl = plan[p.first_long + a + 1] - plan[p.first_long + a];
+    if (nl == 1 || (nl == 0 && gp.accumulate)) return;
+    const GradJob& jb = gp.job[(int)blockIdx.x < blocks0 ? 0 : 1];
+    const int64_t size = (int64_t)gp.rank * jb.cols;
+    const int64_t i = ((int64_t)(blockIdx.x - ((int)blockIdx.x < blocks0 ? 0 : blocks0)) * 256 + threadIdx.x) * 4;
+    if (i >= size) return;
+    f32x4 s = (f32x4)(0.f);
+    const float* part = jb.part + plan[p.first_slot + a] * size + i;
+    for (int u = 0; u < nl; ++u) s += *(const f32x4*)(part + u * size);
+    f32x4* at = (f32x4*)(jb.out + a * size + i);
+    *at = gp.accumulate ? *at + s : s;
+}
+
+bool al(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+int check_shape(const ssd_adapter_shape_t* s) {
+    if (!s) return SSD_ERR_NULL;
+    const int rc = linear_check(s->rows, s->in_dim, s->out_dim, s->x_row_stride, s->out_row_stride);
+    if (rc != SSD_OK) return rc;
+    if (s->dx_row_stride && (s->dx_row_stride < s->in_dim || (s->dx_row_stride & 7))) return SSD_ERR_SHAPE;
+    if (s->rank <= 0 || s->rank > MAX_RANK || s->nadapters <= 0 || s->nadapters > SSD_MAX_ADAPTERS) return SSD_ERR_SHAPE;
+    if (s->rank & 7) return SSD_ERR_DIVISIBILITY;
+    return SSD_OK;
+}
+
+size_t pad(size_t b) { return (b + 255) / 256 * 256; }
+size_t low_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->rows * s->rank * sizeof(float)); }
+size_t part_bytes(const Plan& p, const ssd_adapter_shape_t* s, int cols) { return pad((size_t)most_slots(p) * s->rank * cols * sizeof(float)); }
+
+template <int RT>
+hipError_t launch_grads_rt(const GradParams& gp, const Plan& p, const int* plan, hipStream_t st) {
+    hipLaunchKernelGGL((k_adapter_grads<RT>), dim3(gp.job[0].blocks + gp.job[1].blocks, p.max_long, (gp.rank + 16 * RT - 1) / (16 * RT)), dim3(256), 0, st, gp, p, plan);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace ssdk
+
+using namespace ssdk;
+
+extern "C" size_t ssd_adapter_plan_bytes(int64_t rows, int32_t nadapters) {
+    if (rows < 0 || rows > SSD_MAX_ADAPTER_ROWS || nadapters <= 0 || nadapters > SSD_MAX_ADAPTERS) return 0;
+    return pad((size_t)plan_of(rows, nadapters).words * sizeof(int));
+}
+
+extern "C" int ssd_adapter_plan(int64_t rows, int32_t nadapters, const int32_t* row_adapter, void* plan, size_t plan_bytes, void* hip_stream) {
+    const size_t need = ssd_adapter_plan_bytes(rows, nadapters);
+    if (!need) return SSD_ERR_SHAPE;
+    if (!plan || (rows && !row_adapter)) return SSD_ERR_NULL;
+    if (!al(row_adapter, 4)) return SSD_ERR_ARG;
+    if (!al(plan, 256) || plan_bytes < need) return SSD_ERR_WORKSPACE;
+    const Plan p = plan_of(rows, nadapters);
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipLaunchKernelGGL(k_plan_count, dim3(p.tiles + nadapters + 1), dim3(PTHR), 0, st, p, row_adapter, (int*)plan);
+    hipLaunchKernelGGL(k_plan_rows, dim3(nadapters + 1), dim3(PTHR), 0, st, p, (int*)plan);
+    return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
+}
+
+extern "C" size_t ssd_adapter_workspace_bytes(const ssd_adapter_shape_t* shape, int32_t is_backward) {
+    if (check_shape(shape) != SSD_OK || shape->rows > SSD_MAX_ADAPTER_ROWS) return 0;
+    if (!is_backward) return low_bytes(shape) + 256;
+    const Plan p = plan_of(shape->rows, shape->nadapters);
+    return 2 * low_bytes(shape) + part_bytes(p, shape, shape->in_dim) + part_bytes(p, shape, shape->out_dim) + 256;
+}
+
+extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const void* x, const void* w, const void* a, const void* b,
+                                      const float* scale, const void* plan, void* out, float* hidden, void* workspace,
+                                      size_t workspace_bytes, void* hip_stream) {
+    const int rc = check_shape(shape);
+    if (rc != SSD_OK) return rc;
+    if (shape->rows > SSD_MAX_ADAPTER_ROWS) return SSD_ERR_SHAPE;
+    if (shape->rows == 0) return SSD_OK;
+    if (!x || !w || !a || !b || !scale || !plan || !out) return SSD_ERR_NULL;
+    if (!al(x, 16) || !al(w, 16) || !al(a, 16) || !al(b, 16) || !al(out, 16) || !al(scale, 4) || !al(hidden, 16) || !al(plan, 256)) return SSD_ERR_ARG;
+    if (!hidden && (!workspace || !al(workspace, 256) || workspace_bytes < ssd_adapter_workspace_bytes(shape, 0))) return SSD_ERR_WORKSPACE;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const Plan p = plan_of(shape->rows, shape->nadapters);
+    const int* pl = (const int*)plan;
+    float* low = hidden ? hidden : (float*)workspace;
+    const int64_t ldx = shape->x_row_stride ? shape->x_row_stride : shape->in_dim;
+    const LowParams lp = {(const __bf16*)x, ldx, (const __bf16*)a, scale, low, shape->in_dim, shape->rank};
+    if (launch_low_products<false>(lp, p, pl, st) != hipSuccess) return SSD_ERR_LAUNCH;
+    const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, low, (const bf16_t*)b, shape->rank, shape->out_dim};
+    const hipError_t e = launch_linear_low(false, shape->rows, shape->in_dim, shape->out_dim, x, ldx, w, out,
+                                           shape->out_row_stride ? shape->out_row_stride : shape->out_dim, lr, st);
+    return e == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
+}
+
+extern "C" int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const void* x, const void* w, const void* a, const void* b,
+                                      const float* scale, const void* plan, const void* dout, const float* hidden, void* dx, float* da,
+                                      float* db, void* workspace, size_t workspace_bytes, uint32_t flags, void* hip_stream) {
+    const int rc = check_shape(shape);
+    if (rc != SSD_OK) return rc;
+    if (shape->rows > SSD_MAX_ADAPTER_ROWS) return SSD_ERR_SHAPE;
+    if (flags & ~(uint32_t)SSD_FLAG_ACCUM_PARAM) return SSD_ERR_ARG;
+    if ((da == nullptr) != (db == nullptr)) return SSD_ERR_NULL;
+    hipStream_t st = (hipStream_t)hip_stream;
+    const bool accumulate = flags & SSD_FLAG_ACCUM_PARAM;
+    const size_t size_a = (size_t)shape->nadapters * shape->rank * shape->in_dim, size_b = (size_t)shape->nadapters * shape->rank * shape->out_dim;
+    if (!al(da, 16) || !al(db, 16)) return SSD_ERR_ARG;
+    if (shape->rows == 0) {
+        if (da && !accumulate && (launch_fill_zero(da, size_a, st) != hipSuccess || launch_fill_zero(db, size_b, st) != hipSuccess)) return SSD_ERR_LAUNCH;
+        return SSD_OK;
+    }
+    if (!dx && !da) return SSD_OK;
+    if (!a || !b || !scale || !plan || !dout || (dx && !w) || (da && !x)) return SSD_ERR_NULL;
+    if (!al(x, 16) || !al(w, 16) || !al(a, 16) || !al(b, 16) || !al(dout, 16) || !al(dx, 16) || !al(scale, 4) || !al(hidden, 16) || !al(plan, 256)) return SSD_ERR_ARG;
+    if (!workspace || !al(workspace, 256) || workspace_bytes < ssd_adapter_workspace_bytes(shape, 1)) return SSD_ERR_WORKSPACE;
+    const Plan p = plan_of(shape->rows, shape->nadapters);
+    const int* pl = (const int*)plan;
+    char* ws = (char*)workspace;
+    float *g = (float*)ws, *own_h = (float*)(ws + low_bytes(shape));
+    float *part_a = (float*)(ws + 2 * low_bytes(shape)), *part_b = (float*)((char*)part_a + part_bytes(p, shape, shape->in_dim));
+    const int64_t ldx = shape->x_row_stride ? shape->x_row_stride : shape->in_dim, ldd = shape->out_row_stride ? shape->out_row_stride : shape->out_dim;
+    const LowParams lg = {(const __bf16*)dout, ldd, (const __bf16*)b, scale, g, shape->out_dim, shape->rank};
+    if (launch_low_products<true>(lg, p, pl, st) != hipSuccess) return SSD_ERR_LAUNCH;
+    if (dx) {
+        const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, g, (const bf16_t*)a, shape->rank, shape->in_dim};
+        if (launch_linear_low(true, shape->rows, shape->in_dim, shape->out_dim, dout, ldd, w, dx, shape->dx_row_stride ? shape->dx_row_stride : shape->in_dim, lr, st) != hipSuccess)
+            return SSD_ERR_LAUNCH;
+    }
+    if (!da) return SSD_OK;
+    if (!hidden) {
+        const LowParams lh = {(const __bf16*)x, ldx, (const __bf16*)a, scale, own_h, shape->in_dim, shape->rank};
+        if (launch_low_products<false>(lh, p, pl, st) != hipSuccess) return SSD_ERR_LAUNCH;
+        hidden = own_h;
+    }
+    GradParams gp;
+    gp.job[0] = {(const __bf16*)x, ldx, g, da, part_a, shape->in_dim, (shape->in_dim + GCOLS - 1) / GCOLS};
+    gp.job[1] = {(const __bf16*)dout, ldd, hidden, db, part_b, shape->out_dim, (shape->out_dim + GCOLS - 1) / GCOLS};
+    gp.rank = shape->rank;
+    gp.accumulate = accumulate;
+    const hipError_t e = gp.rank <= 16 ? launch_grads_rt<1>(gp, p, pl, st) : gp.rank <= 32 ? launch_grads_rt<2>(gp, p, pl, st) : launch_grads_rt<4>(gp, p, pl, st);
+    if (e != hipSuccess) return SSD_ERR_LAUNCH;
+    const int64_t b0 = ((int64_t)gp.rank * shape->in_dim + 1023) / 1024, b1 = ((int64_t)gp.rank * shape->out_dim + 1023) / 1024;
+    hipLaunchKernelGGL(k_adapter_grads_sum, dim3((unsigned)(b0 + b1), shape->nadapters), dim3(256), 0, st, gp, p, pl, (int)b0);
+    return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
+}

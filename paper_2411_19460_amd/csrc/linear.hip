@@ -352,8 +352,77 @@ struct Big {
 
 extern __shared__ __attribute__((aligned(1024))) char lds[];  // the K steps in flight; at the end the patches of the result
 
-template <bool AK, bool BK, int WJ>
-__device__ __forceinline__ void gemm_tile(const GemmParams& gp, int id) {
+// The low-rank term of a tile, C[t, :] += low[t, :] up_a for the adapter a of each row t: `up_a` is staged as the operand B is, `low`
+// like A, rounded to bf16 (the result is rounded to bf16 as well, and the term is the smaller part of it).  A row keeps the products with
+// its own adapter alone, by a selection and not by zeros in `low`: an infinity in one adapter stays with the rows that have it.  Only
+// where the whole tile has one adapter do the products go straight into its accumulators.
+template <bool BK, int WJ>
+__device__ __forceinline__ void add_low_rank(Big<true, BK, WJ>& G, const BigCtx& cx, const GemmParams& gp, const LowRankTerm& lr, int tm, int m0, int n0) {
+    typedef Tile<256, true> TA;
+    typedef Tile<64 * WJ, BK> TB;
+    const int listed = lr.tile_n[tm], nu = listed & 0xffff;
+    const bool whole = listed & 0x10000;
+    char *la = G.lds, *lb = G.lds + Big<true, BK, WJ>::NA * TA::BYTES;
+    int of_row[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = m0 + cx.wm * 64 + i * 16 + (cx.lane & 15);
+        of_row[i] = m < gp.M ? lr.ids[m] : -1;
+    }
+    for (int k0 = 0; k0 < lr.rank; k0 += BKK) {
+        const int left = lr.rank - k0, halves = left > 32 ? 2 : 1;
+        for (int u = 0; u < nu; ++u) {
+            const int64_t a = lr.tile_a[(int64_t)tm * 256 + u];
+            __syncthreads();  // the operands before these have been read
+            if (u == 0) {
+#pragma unroll
+                for (int i = 0; i < TA::LOADS; ++i) {
+                    const int r = TA::row(cx.tid) + TA::RSTEP * i, c = TA::piece(cx.tid) * 8;
+                    bf16x8 v;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = (__bf16)0.f;
+                    if (m0 + r < gp.M && c < left) {
+                        const f32x4* q = (const f32x4*)(lr.low + (int64_t)(m0 + r) * lr.rank + k0 + c);
+                        const f32x4 q0 = q[0], q1 = q[1];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = (__bf16)q0[e], v[4 + e] = (__bf16)q1[e];
+                    }
+                    *(bf16x8*)(la + i * 16 * GTHR + cx.tid * 16) = v;
+                }
+            }
+            const bf16_t* up = lr.up + a * lr.rank * lr.width + (BK ? (int64_t)n0 * lr.rank + k0 : (int64_t)k0 * lr.width + n0);
+            TB::load_part(up, BK ? lr.rank : lr.width, gp.N - n0, left, lb, cx.tid);
+            __syncthreads();
+            if (u == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks)
+                        if (ks < halves) G.a[i][ks] = TA::operand(la, cx.wm * 64 + i * 16, ks, cx.lane);
+            }
+#pragma unroll
+            for (int j = 0; j < 2 * WJ; ++j) {
+                f32x4 t[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[i] = (f32x4)(0.f);
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (ks < halves) {
+                        const bf16x8 b = TB::operand(lb, cx.wn * 32 * WJ + j * 16, ks, cx.lane);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, G.a[i][ks], t[i], 0, 0, 0);
+                    }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) G.acc[i][j][e] += whole || of_row[i] == (int)a ? t[i][e] : 0.f;
+            }
+        }
+    }
+}
+
+template <bool AK, bool BK, int WJ, bool LOW = false>
+__device__ __forceinline__ void gemm_tile(const GemmParams& gp, int id, const LowRankTerm* lr = nullptr) {
     constexpr int BM = 256, BN = 64 * WJ;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn;
@@ -396,6 +465,7 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& gp, int id) {
     if (direct)
         for (; k0 + (Gemm::AHEAD_B + 1) * BKK <= gp.K; k0 += BKK) G.template step<true>(cx, k0, true);
     for (; k0 < gp.K; k0 += BKK) G.template step<false>(cx, k0, direct);
+    if constexpr (LOW) add_low_rank<BK, WJ>(G, cx, gp, *lr, tm, m0, n0);
 
     if (gp.c_f32) {
         store_acc_f32<WJ>(gp, acc, m0 + wm * 64, n0 + wn * 32 * WJ, lane);
@@ -447,6 +517,17 @@ __global__ __launch_bounds__(GTHR, 1) void k_gemm_grads(GemmParams px, GemmParam
     const int id = second ? blockIdx.x - first : blockIdx.x;
     if (second == (dw_first != 0)) gemm_tile<true, false, WX>(px, id);
     else gemm_tile<false, false, WW>(pw, id);
+}
+
+// A product with a low-rank term: the forward one (BK) or that of the input's gradient.
+template <bool BK, int WJ>
+__global__ __launch_bounds__(GTHR, 1) void k_gemm_low(GemmParams gp, LowRankTerm lr) {
+    gemm_tile<true, BK, WJ, true>(gp, blockIdx.x, &lr);
+}
+template <int W1, int W2>
+__global__ __launch_bounds__(GTHR, 1) void k_gemm_low_mixed(GemmParams p1, GemmParams p2, LowRankTerm lr, LowRankTerm lr2, int first) {
+    if ((int)blockIdx.x < first) gemm_tile<true, true, W1, true>(p1, blockIdx.x, &lr);
+    else gemm_tile<true, true, W2, true>(p2, blockIdx.x - first, &lr2);
 }
 
 bool ok_ptr(const void* p) { return p && ((uintptr_t)p & 15) == 0; }
@@ -590,7 +671,61 @@ int check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ld
     return SSD_OK;
 }
 
+template <bool BK, int WJ>
+hipError_t launch_low(GemmParams gp, const LowRankTerm& lr, hipStream_t st) {
+    constexpr int LDS = big_lds<true, BK, WJ>();
+    static bool raised[64];
+    const hipError_t e = allow_lds((const void*)k_gemm_low<BK, WJ>, LDS, raised);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_gemm_low<BK, WJ>), dim3(set_tiles(gp, WJ)), dim3(GTHR), LDS, st, gp, lr);
+    return hipGetLastError();
+}
+
+template <int W1, int W2>
+hipError_t launch_low_mixed(GemmParams gp, int n1, const LowRankTerm& lr, hipStream_t st) {
+    constexpr int L1 = big_lds<true, true, W1>(), L2 = big_lds<true, true, W2>(), LDS = L1 > L2 ? L1 : L2;
+    static bool raised[64];
+    const hipError_t e = allow_lds((const void*)k_gemm_low_mixed<W1, W2>, LDS, raised);
+    if (e != hipSuccess) return e;
+    GemmParams p2 = gp;
+    LowRankTerm lr2 = lr;
+    gp.N = n1;
+    p2.N -= n1;
+    p2.B += (int64_t)n1 * gp.ldb;
+    p2.C = (bf16_t*)gp.C + n1;
+    lr2.up += (int64_t)n1 * lr.rank;
+    const int t1 = set_tiles(gp, W1), t2 = set_tiles(p2, W2);
+    hipLaunchKernelGGL((k_gemm_low_mixed<W1, W2>), dim3(t1 + t2), dim3(GTHR), LDS, st, gp, p2, lr, lr2, t1);
+    return hipGetLastError();
+}
+
 }  // namespace
+
+int linear_check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ldo) { return check(rows, in_dim, out_dim, ldx, ldo); }
+
+hipError_t launch_linear_low(bool input_grad, int64_t rows, int in_dim, int out_dim, const void* x, int64_t ldx, const void* w, void* out, int64_t ldo,
+                             const LowRankTerm& lr, hipStream_t st) {
+    GemmParams gp;
+    memset(&gp, 0, sizeof(gp));
+    gp.A = (const bf16_t*)x;
+    gp.B = (const bf16_t*)w;  // [out_dim, in_dim]: k-major for the forward product, k as the row index for the gradient
+    gp.C = out;
+    gp.lda = ldx;
+    gp.ldb = in_dim;
+    gp.ldc = ldo;
+    gp.M = (int)rows;
+    gp.N = input_grad ? in_dim : out_dim;
+    gp.K = input_grad ? out_dim : in_dim;
+    if (input_grad) {
+        int wx, ww;
+        bool first;
+        backward_widths(&gp, nullptr, wx, ww, first);
+        return wx == 4 ? launch_low<false, 4>(gp, lr, st) : launch_low<false, 2>(gp, lr, st);
+    }
+    const ForwardPlan f = forward_plan(gp);
+    if (f.n1 < gp.N) return f.w == 4 ? launch_low_mixed<4, 3>(gp, f.n1, lr, st) : launch_low_mixed<3, 2>(gp, f.n1, lr, st);
+    return f.w == 4 ? launch_low<true, 4>(gp, lr, st) : f.w == 3 ? launch_low<true, 3>(gp, lr, st) : launch_low<true, 2>(gp, lr, st);
+}
 }  // namespace ssdk
 
 using namespace ssdk;

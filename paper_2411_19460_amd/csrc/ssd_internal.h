@@ -346,6 +346,22 @@ struct SideStream {
 };
 SideStream* side_stream();
 
+// Low-rank term of a product (adapters.hip -> linear.hip): C[t, :] += low[t, :] up_a, a = ids[t] the adapter of row t (-1: none).
+// ids and the adapters that each tile of LOW_TILE rows meets come from the plan of the rows.
+constexpr int LOW_TILE = 256;
+struct LowRankTerm {
+    const int* ids;     // [rows]
+    const int* tile_n;  // [tiles]: how many adapters; bit 16: one, and every row of the tile has it
+    const int* tile_a;  // [tiles][LOW_TILE]: which, ascending
+    const float* low;   // [rows, rank]
+    const bf16_t* up;   // [adapters][width][rank] (forward) or [adapters][rank][width] (gradient of the input)
+    int rank, width;    // width: columns of the whole product
+};
+int linear_check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ldo);  // sizes and strides, as ssd_linear_fwd
+// out = x w^T + low up (rows of in_dim -> out_dim), or with input_grad out = x w + low up (rows of out_dim -> in_dim)
+hipError_t launch_linear_low(bool input_grad, int64_t rows, int in_dim, int out_dim, const void* x, int64_t ldx, const void* w, void* out, int64_t ldo,
+                             const LowRankTerm& lr, hipStream_t st);
+
 // Generation (few_rows.hip): products and the block's middle steps for at most FEW_ROWS tokens, bf16 storage.
 constexpr int FEW_ROWS = 16;
 // Up to this many rows the product runs on the vector ALUs, above on the matrix cores.
