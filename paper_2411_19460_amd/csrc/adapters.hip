@@ -90,14 +90,14 @@ __global__ __launch_bounds__(PTHR) void k_plan_count(Plan p, const int* row_adap
         __syncthreads();
         bool first = a >= 0;
         for (int j = 0; j < tid; ++j) first = first && lds[j] != a;
-        const int whole = __syncthreads_and(a == -2 || a == lds[0]);
+        __syncthreads();
         lds[tid] = first ? a : 0x7fffffff;
         __syncthreads();
         int place = 0;
         for (int j = 0; j < LOW_TILE; ++j) place += lds[j] < a;
         if (first) plan[p.tile_a + (int64_t)blockIdx.x * LOW_TILE + place] = a;
         const int listed = block_sum(first, lds);
-        if (tid == 0) plan[p.tile_n + blockIdx.x] = listed | (whole && listed == 1 ? 0x10000 : 0);
+        if (tid == 0) plan[p.tile_n + blockIdx.x] = listed;
         return;
     }
     const int mine = blockIdx.x - p.tiles;
@@ -274,10 +274,32 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* rows, i
     }
 }
 
+// a [adapters][rank][in_dim] with the rank contiguous, for the product that joins dx (see add_low_rank): pieces of 64 columns of an
+// adapter, eight ranks at a time.
+struct TurnJob {
+    const __bf16* a;
+    __bf16* to;   // [adapters][in_dim][rank]; null: no such job
+    int in_dim, rank, blocks;  // blocks: of 64 columns, times adapters
+};
+__device__ __forceinline__ void turn_piece(const TurnJob& tj, const Plan& p, const int* plan, int id) {
+    const int per = (tj.in_dim + 63) / 64, a = id / per, c = (id - a * per) * 64 + (threadIdx.x & 63);
+    if (plan[p.start + a] == plan[p.start + a + 1] || c >= tj.in_dim) return;  // nobody has it
+    for (int r = 8 * (threadIdx.x >> 6); r < tj.rank; r += 8 * LWAVES) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tj.a[((int64_t)a * tj.rank + r + e) * tj.in_dim + c];
+        *(bf16x8*)(tj.to + ((int64_t)a * tj.in_dim + c) * tj.rank + r) = v;
+    }
+}
+
 template <int RT, bool KROW>
-__global__ __launch_bounds__(64 * LWAVES) void k_low(LowParams lp, Plan p, const int* plan) {
+__global__ __launch_bounds__(64 * LWAVES) void k_low(LowParams lp, Plan p, const int* plan, TurnJob tj) {
     extern __shared__ __attribute__((aligned(16))) char low_lds_mem[];
-    const int u = blockIdx.x;
+    if (KROW && (int)blockIdx.x < tj.blocks) {
+        if (blockIdx.y == 0) turn_piece(tj, p, plan, blockIdx.x);
+        return;
+    }
+    const int u = blockIdx.x - (KROW ? tj.blocks : 0);
     if (u >= plan[0]) return;
     const int a = plan[p.short_a + u], first = plan[p.start + a] + SHORT_UNIT * (u - plan[p.first_short + a]);
     const int left = plan[p.start + a + 1] - first, cnt = left < SHORT_UNIT ? left : SHORT_UNIT, r0 = blockIdx.y * 16 * RT;
@@ -292,7 +314,7 @@ __global__ __launch_bounds__(64 * LWAVES) void k_low(LowParams lp, Plan p, const
 }
 
 template <int RT, bool KROW>
-hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, hipStream_t st) {
+hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, const TurnJob& tj, hipStream_t st) {
     constexpr int LDS = low_lds<RT, KROW>();
     static bool raised[64];
     if (LDS > 65536) {
@@ -304,15 +326,15 @@ hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, hi
             raised[dev] = true;
         }
     }
-    hipLaunchKernelGGL((k_low<RT, KROW>), dim3(p.max_short, (lp.rank + 16 * RT - 1) / (16 * RT)), dim3(64 * LWAVES), LDS, st, lp, p, plan);
+    hipLaunchKernelGGL((k_low<RT, KROW>), dim3(p.max_short + tj.blocks, (lp.rank + 16 * RT - 1) / (16 * RT)), dim3(64 * LWAVES), LDS, st, lp, p, plan, tj);
     return hipGetLastError();
 }
 
 template <bool KROW>
-hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* plan, hipStream_t st) {
-    if (lp.rank <= 16) return launch_low_rt<1, KROW>(lp, p, plan, st);
-    if (lp.rank <= 32) return launch_low_rt<2, KROW>(lp, p, plan, st);
-    return launch_low_rt<4, KROW>(lp, p, plan, st);
+hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* plan, const TurnJob& tj, hipStream_t st) {
+    if (lp.rank <= 16) return launch_low_rt<1, KROW>(lp, p, plan, tj, st);
+    if (lp.rank <= 32) return launch_low_rt<2, KROW>(lp, p, plan, tj, st);
+    return launch_low_rt<4, KROW>(lp, p, plan, tj, st);
 }
 
 // ---- the adapters' gradients ----
@@ -462,6 +484,7 @@ int check_shape(const ssd_adapter_shape_t* s) {
 
 size_t pad(size_t b) { return (b + 255) / 256 * 256; }
 size_t low_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->rows * s->rank * sizeof(float)); }
+size_t turned_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->nadapters * s->rank * s->in_dim * 2); }
 size_t part_bytes(const Plan& p, const ssd_adapter_shape_t* s, int cols) { return pad((size_t)most_slots(p) * s->rank * cols * sizeof(float)); }
 
 template <int RT>
@@ -497,7 +520,7 @@ extern "C" size_t ssd_adapter_workspace_bytes(const ssd_adapter_shape_t* shape, 
     if (check_shape(shape) != SSD_OK || shape->rows > SSD_MAX_ADAPTER_ROWS) return 0;
     if (!is_backward) return low_bytes(shape) + 256;
     const Plan p = plan_of(shape->rows, shape->nadapters);
-    return 2 * low_bytes(shape) + part_bytes(p, shape, shape->in_dim) + part_bytes(p, shape, shape->out_dim) + 256;
+    return 2 * low_bytes(shape) + turned_bytes(shape) + part_bytes(p, shape, shape->in_dim) + part_bytes(p, shape, shape->out_dim) + 256;
 }
 
 extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const void* x, const void* w, const void* a, const void* b,
@@ -516,7 +539,7 @@ extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const vo
     float* low = hidden ? hidden : (float*)workspace;
     const int64_t ldx = shape->x_row_stride ? shape->x_row_stride : shape->in_dim;
     const LowParams lp = {(const __bf16*)x, ldx, (const __bf16*)a, scale, low, shape->in_dim, shape->rank};
-    if (launch_low_products<false>(lp, p, pl, st) != hipSuccess) return SSD_ERR_LAUNCH;
+    if (launch_low_products<false>(lp, p, pl, TurnJob{}, st) != hipSuccess) return SSD_ERR_LAUNCH;
     const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, low, (const bf16_t*)b, shape->rank, shape->out_dim};
     const hipError_t e = launch_linear_low(false, shape->rows, shape->in_dim, shape->out_dim, x, ldx, w, out,
                                            shape->out_row_stride ? shape->out_row_stride : shape->out_dim, lr, st);
@@ -547,19 +570,22 @@ extern "C" int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const vo
     const int* pl = (const int*)plan;
     char* ws = (char*)workspace;
     float *g = (float*)ws, *own_h = (float*)(ws + low_bytes(shape));
-    float *part_a = (float*)(ws + 2 * low_bytes(shape)), *part_b = (float*)((char*)part_a + part_bytes(p, shape, shape->in_dim));
+    __bf16* turned = (__bf16*)(ws + 2 * low_bytes(shape));
+    float *part_a = (float*)((char*)turned + turned_bytes(shape)), *part_b = (float*)((char*)part_a + part_bytes(p, shape, shape->in_dim));
     const int64_t ldx = shape->x_row_stride ? shape->x_row_stride : shape->in_dim, ldd = shape->out_row_stride ? shape->out_row_stride : shape->out_dim;
     const LowParams lg = {(const __bf16*)dout, ldd, (const __bf16*)b, scale, g, shape->out_dim, shape->rank};
-    if (launch_low_products<true>(lg, p, pl, st) != hipSuccess) return SSD_ERR_LAUNCH;
+    TurnJob tj = {};
+    if (dx) tj = {(const __bf16*)a, turned, shape->in_dim, shape->rank, shape->nadapters * ((shape->in_dim + 63) / 64)};
+    if (launch_low_products<true>(lg, p, pl, tj, st) != hipSuccess) return SSD_ERR_LAUNCH;
     if (dx) {
-        const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, g, (const bf16_t*)a, shape->rank, shape->in_dim};
+        const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, g, (const bf16_t*)turned, shape->rank, shape->in_dim};
         if (launch_linear_low(true, shape->rows, shape->in_dim, shape->out_dim, dout, ldd, w, dx, shape->dx_row_stride ? shape->dx_row_stride : shape->in_dim, lr, st) != hipSuccess)
             return SSD_ERR_LAUNCH;
     }
     if (!da) return SSD_OK;
     if (!hidden) {
         const LowParams lh = {(const __bf16*)x, ldx, (const __bf16*)a, scale, own_h, shape->in_dim, shape->rank};
-        if (launch_low_products<false>(lh, p, pl, st) != hipSuccess) return SSD_ERR_LAUNCH;
+        if (launch_low_products<false>(lh, p, pl, TurnJob{}, st) != hipSuccess) return SSD_ERR_LAUNCH;
         hidden = own_h;
     }
     GradParams gp;

@@ -16,6 +16,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include "low_rank.h"
 #include "mfma_common.h"
 
 namespace ssdk {
@@ -272,8 +273,9 @@ struct Big {
         }
     }
 
-    // Fills the buffers and reads the first operands.
-    __device__ __forceinline__ void start(const BigCtx& cx, bool direct) {
+    // Fills the buffers and reads the first operands; `meanwhile` runs while the first loads are under way.
+    template <typename F>
+    __device__ __forceinline__ void start(const BigCtx& cx, bool direct, F meanwhile) {
         a0 = b0 = 0;
         load_step_a(cx, 0, 0, direct);
         load_step_b(cx, 0, 0, direct);
@@ -281,6 +283,7 @@ struct Big {
         load_step_b(cx, BKK, 1, direct);
         if (NA == 3) load_step_a(cx, 2 * BKK, 2, direct);
         load_step_b(cx, 2 * BKK, 2, direct);
+        meanwhile();
         if (direct && 3 * BKK <= cx.K) wait_and_meet<(NA - 1) * TA::LOADS + 2 * TB::LOADS>();
         else wait_and_meet<0>();
 #pragma unroll
@@ -352,75 +355,6 @@ struct Big {
 
 extern __shared__ __attribute__((aligned(1024))) char lds[];  // the K steps in flight; at the end the patches of the result
 
-// The low-rank term of a tile, C[t, :] += low[t, :] up_a for the adapter a of each row t: `up_a` is staged as the operand B is, `low`
-// like A, rounded to bf16 (the result is rounded to bf16 as well, and the term is the smaller part of it).  A row keeps the products with
-// its own adapter alone, by a selection and not by zeros in `low`: an infinity in one adapter stays with the rows that have it.  Only
-// where the whole tile has one adapter do the products go straight into its accumulators.
-template <bool BK, int WJ>
-__device__ __forceinline__ void add_low_rank(Big<true, BK, WJ>& G, const BigCtx& cx, const GemmParams& gp, const LowRankTerm& lr, int tm, int m0, int n0) {
-    typedef Tile<256, true> TA;
-    typedef Tile<64 * WJ, BK> TB;
-    const int listed = lr.tile_n[tm], nu = listed & 0xffff;
-    const bool whole = listed & 0x10000;
-    char *la = G.lds, *lb = G.lds + Big<true, BK, WJ>::NA * TA::BYTES;
-    int of_row[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = m0 + cx.wm * 64 + i * 16 + (cx.lane & 15);
-        of_row[i] = m < gp.M ? lr.ids[m] : -1;
-    }
-    for (int k0 = 0; k0 < lr.rank; k0 += BKK) {
-        const int left = lr.rank - k0, halves = left > 32 ? 2 : 1;
-        for (int u = 0; u < nu; ++u) {
-            const int64_t a = lr.tile_a[(int64_t)tm * 256 + u];
-            __syncthreads();  // the operands before these have been read
-            if (u == 0) {
-#pragma unroll
-                for (int i = 0; i < TA::LOADS; ++i) {
-                    const int r = TA::row(cx.tid) + TA::RSTEP * i, c = TA::piece(cx.tid) * 8;
-                    bf16x8 v;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = (__bf16)0.f;
-                    if (m0 + r < gp.M && c < left) {
-                        const f32x4* q = (const f32x4*)(lr.low + (int64_t)(m0 + r) * lr.rank + k0 + c);
-                        const f32x4 q0 = q[0], q1 = q[1];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = (__bf16)q0[e], v[4 + e] = (__bf16)q1[e];
-                    }
-                    *(bf16x8*)(la + i * 16 * GTHR + cx.tid * 16) = v;
-                }
-            }
-            const bf16_t* up = lr.up + a * lr.rank * lr.width + (BK ? (int64_t)n0 * lr.rank + k0 : (int64_t)k0 * lr.width + n0);
-            TB::load_part(up, BK ? lr.rank : lr.width, gp.N - n0, left, lb, cx.tid);
-            __syncthreads();
-            if (u == 0) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks)
-                        if (ks < halves) G.a[i][ks] = TA::operand(la, cx.wm * 64 + i * 16, ks, cx.lane);
-            }
-#pragma unroll
-            for (int j = 0; j < 2 * WJ; ++j) {
-                f32x4 t[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t[i] = (f32x4)(0.f);
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks)
-                    if (ks < halves) {
-                        const bf16x8 b = TB::operand(lb, cx.wn * 32 * WJ + j * 16, ks, cx.lane);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) t[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, G.a[i][ks], t[i], 0, 0, 0);
-                    }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) G.acc[i][j][e] += whole || of_row[i] == (int)a ? t[i][e] : 0.f;
-            }
-        }
-    }
-}
-
 template <bool AK, bool BK, int WJ, bool LOW = false>
 __device__ __forceinline__ void gemm_tile(const GemmParams& gp, int id, const LowRankTerm* lr = nullptr) {
     constexpr int BM = 256, BN = 64 * WJ;
@@ -460,12 +394,16 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& gp, int id, const Lo
     const int lane = cx.lane, wm = cx.wm, wn = cx.wn;
     // strides beyond what 32-bit offsets reach: every step goes through registers
     const bool direct = gp.lda <= MAX_LD && gp.ldb <= MAX_LD;
-    G.start(cx, direct);
+    G.start(cx, direct, [&] {
+        if constexpr (LOW) {
+            add_low_rank<4, 2 * WJ>(acc, *lr, m0 + wm * 64, gp.M, n0 + wn * 32 * WJ, gp.N, lane, 0, 1);
+            wait_loads();  // for the compiler: it would wait in every K step for what it thinks may still be under way from here
+        }
+    });
     int k0 = 0;
     if (direct)
         for (; k0 + (Gemm::AHEAD_B + 1) * BKK <= gp.K; k0 += BKK) G.template step<true>(cx, k0, true);
     for (; k0 < gp.K; k0 += BKK) G.template step<false>(cx, k0, direct);
-    if constexpr (LOW) add_low_rank<BK, WJ>(G, cx, gp, *lr, tm, m0, n0);
 
     if (gp.c_f32) {
         store_acc_f32<WJ>(gp, acc, m0 + wm * 64, n0 + wn * 32 * WJ, lane);

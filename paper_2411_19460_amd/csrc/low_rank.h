@@ -1,0 +1,65 @@
+// The low-rank term of a product on the matrix cores: what the rows' adapters add to a tile of x w^T, straight from memory to operands.
+#pragma once
+#include "mfma_common.h"
+
+namespace ssdk {
+
+// acc[i][j] += low[t, :] up_a^T for the rows t = m0 + 16 i + lane % 16 and the columns n0 + 16 j + 4 (lane / 16) + 0..3, a the adapter
+// of row t: the accumulator layout of 16 x 16 x 32 MFMAs that are issued with the columns' operand first.  The rows lie in one tile of
+// the plan (LOW_TILE).  Both operands have the rank contiguous, so a lane's eight values are one piece of memory and nothing goes
+// through LDS.  `low` is rounded to bf16: the result is, and the term is the smaller part of it.  A row keeps the products with its own
+// adapter alone, by a selection and not by zeros in `low`: an infinity in one adapter stays with the rows that have it.  Of the
+// tile's adapters this call takes numbers u0, u0 + ustep, ...
+template <int MT, int NT>
+static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], const LowRankTerm& lr, int m0, int M, int n0, int N, int lane, int u0, int ustep) {
+    using namespace mf;
+    const int tile = m0 / LOW_TILE, nu = lr.tile_n[tile], q = lane >> 4, l16 = lane & 15;
+    if (u0 >= nu) return;
+    const int* list = lr.tile_a + (int64_t)tile * LOW_TILE;
+    int of_row[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int m = m0 + 16 * i + l16;
+        of_row[i] = m < M ? lr.ids[m] : -1;
+    }
+    for (int k0 = 0; k0 < lr.rank; k0 += 32) {
+        const int k = k0 + 8 * q;
+        const bool in = k < lr.rank;
+        bf16x8 a[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            a[i] = (bf16x8)((__bf16)0.f);
+            if (in && of_row[i] >= 0) {
+                const f32x4* p = (const f32x4*)(lr.low + (int64_t)(m0 + 16 * i + l16) * lr.rank + k);
+                const f32x4 p0 = p[0], p1 = p[1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[i][e] = (__bf16)p0[e], a[i][4 + e] = (__bf16)p1[e];
+            }
+        }
+        for (int u = u0; u < nu; u += ustep) {
+            const int ad = list[u];
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) any = any || of_row[i] == ad;
+            if (!__any(any)) continue;
+            const bf16_t* up = lr.up + (int64_t)ad * lr.rank * lr.width + k;
+            bf16x8 b[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int n = n0 + 16 * j + l16;
+                b[j] = (bf16x8)((__bf16)0.f);
+                if (in && n < N) b[j] = *(const bf16x8*)(up + (int64_t)n * lr.rank);
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], (f32x4)(0.f), 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] += of_row[i] == ad ? t[e] : 0.f;
+                }
+        }
+    }
+}
+
+}  // namespace ssdk

@@ -351,10 +351,10 @@ SideStream* side_stream();
 constexpr int LOW_TILE = 256;
 struct LowRankTerm {
     const int* ids;     // [rows]
-    const int* tile_n;  // [tiles]: how many adapters; bit 16: one, and every row of the tile has it
+    const int* tile_n;  // [tiles]: how many adapters
     const int* tile_a;  // [tiles][LOW_TILE]: which, ascending
     const float* low;   // [rows, rank]
-    const bf16_t* up;   // [adapters][width][rank] (forward) or [adapters][rank][width] (gradient of the input)
+    const bf16_t* up;   // [adapters][width][rank]
     int rank, width;    // width: columns of the whole product
 };
 int linear_check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ldo);  // sizes and strides, as ssd_linear_fwd
