@@ -8,6 +8,7 @@
 //   k_linear_few<1>  out = RMSNorm(g) norm_w W_out^T (+ the residual)
 // With more rows (several sequences generated together) the per-row arithmetic would bound the products, which then
 // run as small MFMAs (k_linear_few_mfma): three launches as well.
+#include "low_rank.h"
 #include "ssd_internal.h"
 
 namespace ssdk {
@@ -81,6 +82,7 @@ struct FewOperands {
     const float *conv_w, *conv_b, *dt_bias;
     int off_xbc, off_dt, conv_dim;
     int ks, cols;  // waves of a workgroup, columns of one
+    LowRankTerm low;  // products with a low-rank term: one more wave a workgroup works it out while the others stream w
     bool stream;  // w by streaming loads
 };
 
@@ -162,12 +164,23 @@ __device__ __forceinline__ float four_sums(const float (&a)[4]) {
 // Longer rows than the waves have pieces go by in turns (two pieces of two rows to a wave do not fit the registers: 76 to 148 bytes of
 // scratch a lane, and a step of 96 heads, whose d_inner is 6144, took 8 % longer).  STEP: with the convolution step (fo.cs).  Template
 // arguments like MODE: a branch around loads ends in a wait for them.
-template <int MODE, int R, bool STEP, bool STREAM>
+template <int MODE, int R, bool STEP, bool STREAM, bool LOW = false>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(FewParams fp, FewOperands fo, int cols) {
     extern __shared__ float few_sums[];  // [columns, whole fours][R][NW], then the squares [R][NW]
     const int NW = fo.ks, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = blockIdx.x * cols, nc = fp.N - n0 < cols ? fp.N - n0 : cols, nb = (nc + 3) >> 2;
     float *red = few_sums, *sq = few_sums + ((cols + 3) & ~3) * R * NW;
+    if (LOW && w == NW) {  // sq: [columns, whole sixteens][R]
+        for (int c = 0; c < nc; c += 16) {
+            mf::f32x4 acc[1][1] = {{(mf::f32x4)(0.f)}};
+            add_low_rank<1, 1, 2>(acc, fo.low, 0, fp.rows, n0 + c, n0 + nc, lane, 0, 1);
+            if ((lane & 15) < R)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sq[(c + 4 * (lane >> 4) + e) * R + (lane & 15)] = acc[0][0][e];
+        }
+        __syncthreads();
+        return;
+    }
     // columns and pieces beyond the end: nothing is fetched, zeros come back
     const uint32_t rowbytes = (uint32_t)fp.K * 2, bytes = (uint32_t)nc * rowbytes;
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void*)(fp.w + (int64_t)n0 * fp.K), 0, bytes, 0x00020000);
@@ -269,6 +282,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(FewParams fp, Few
             if (MODE) q2 += sq[r * NW + q];
         }
         const int n = n0 + c;
+        if (LOW) v += sq[c * R + r];
         if (MODE) v *= rsqrtf(q2 / (float)fp.K + fp.eps);
         if (fp.res) v += t == tid ? res : (float)fp.res[r * fp.ldres + n];
         const __bf16 ob = (__bf16)v;
@@ -283,6 +297,14 @@ hipError_t launch_few_kernel(const FewParams& fp, const FewOperands& fo, int col
     const size_t lds = (size_t)((cols + 3) / 4 * 4 + 1) * (fp.rows <= 1 ? 1 : FEW_ROWS_VALU) * fo.ks * sizeof(float);  // 49 KB at most
     if (fp.rows <= 1) hipLaunchKernelGGL((k_linear_few<MODE, 1, STEP, STREAM>), grid, block, lds, st, fp, fo, cols);
     else hipLaunchKernelGGL((k_linear_few<MODE, FEW_ROWS_VALU, STEP, STREAM>), grid, block, lds, st, fp, fo, cols);
+    return hipGetLastError();
+}
+
+hipError_t launch_few_low(const FewParams& fp, const FewOperands& fo, int cols, hipStream_t st) {
+    const dim3 grid((unsigned)((fp.N + cols - 1) / cols)), block(64 * (fo.ks + 1));
+    const size_t lds = (size_t)((cols + 3) / 4 * 4 * fo.ks + (cols + 15) / 16 * 16) * (fp.rows <= 1 ? 1 : FEW_ROWS_VALU) * sizeof(float);
+    if (fp.rows <= 1) hipLaunchKernelGGL((k_linear_few<0, 1, false, false, true>), grid, block, lds, st, fp, fo, cols);
+    else hipLaunchKernelGGL((k_linear_few<0, FEW_ROWS_VALU, false, false, true>), grid, block, lds, st, fp, fo, cols);
     return hipGetLastError();
 }
 
@@ -310,7 +332,8 @@ hipError_t launch_few(const FewParams& fp, FewOperands fo, hipStream_t st) {
     const int pieces = (fp.K + FEW_PIECE - 1) / FEW_PIECE;
     const bool alone = MODE == 0 && !fo.cs, two = fp.rows > 1, wide = fp.N >= 12288;
     const bool small = alone && pieces > 1 && (!two || wide || pieces > FEW_WAVES);
-    const int most = !small ? FEW_WAVES : two && wide ? (pieces % 5 ? 4 : 5) : pieces > FEW_WAVES ? 8 : FEW_WAVES, turns = (pieces + most - 1) / most;
+    const int all = fo.low.up ? FEW_WAVES - 1 : FEW_WAVES;  // (of a workgroup's waves one may be the low-rank term's)
+    const int most = !small ? all : two && wide ? (pieces % 5 ? 4 : 5) : pieces > all ? 8 : all, turns = (pieces + most - 1) / most;
     fo.ks = (pieces + turns - 1) / turns;
     int cols = 4;
     if (small) {
@@ -321,6 +344,7 @@ hipError_t launch_few(const FewParams& fp, FewOperands fo, hipStream_t st) {
         cols = even_columns(fp.N, fp.K, 256 * (((alone && (!two || pieces <= 5) ? 16 : 10) + fo.ks / 2) / fo.ks), FEW_COLS);
         cols = cols < 4 ? 4 : cols;
     }
+    if (fo.low.up) return launch_few_low(fp, fo, cols, st);
     if (fo.stream) return fo.cs ? launch_few_kernel<MODE, true, true>(fp, fo, cols, st) : launch_few_kernel<MODE, false, true>(fp, fo, cols, st);
     return fo.cs ? launch_few_kernel<MODE, true, false>(fp, fo, cols, st) : launch_few_kernel<MODE, false, false>(fp, fo, cols, st);
 }
@@ -374,7 +398,7 @@ static_assert(10 * 16 * WPITCH + mfma_tiles(10) * 10 * 1024 <= MFMA_WAVES * 16 *
 // PPW: pieces of a wave that it keeps operands of; longer rows go by in turns (SRC 1: one, two of them and what their
 // normalisation takes do not fit the registers).  The first of w of a turn is asked for in front of the last tile of the turn before: with three
 // rows 5120 x 50288 at its best split 89 us, 94 where it was asked for behind it.
-template <int SRC, bool STEP, int PARTS, bool STREAM, int PPW, bool TURNS>
+template <int SRC, bool STEP, int PARTS, bool STREAM, int PPW, bool TURNS, bool LOW = false>
 __global__ __launch_bounds__(MFMA_WAVES * 64) void k_linear_few_mfma(FewParams fp, FewOperands fo) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int KS = fo.ks, nthr = 64 * KS, tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -383,6 +407,16 @@ __global__ __launch_bounds__(MFMA_WAVES * 64) void k_linear_few_mfma(FewParams f
     float* part = (float*)(lds + KS * 16 * WPITCH);  // [tiles][KS][256]
     float* rs = part + tiles * KS * 256;             // [groups][16]: 1 / rms, or (one group) [16][17]: shares of the squares
     const int col = lane & 15, kq = lane >> 4;   // operand lanes: row of x / column of w, quarter of a 32-wide k step
+    if (LOW && wv == KS) {  // rs: [tiles][256], laid out as a wave's partial tile
+        for (int t = 0; t < tiles; ++t) {
+            mf::f32x4 acc[1][1] = {{(mf::f32x4)(0.f)}};
+            add_low_rank<1, 1, 8>(acc, fo.low, 0, fp.rows, n0 + 16 * t, n0 + ncols, lane, 0, 1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rs[t * 256 + 4 * (4 * kq + e + 16 * (col >> 2)) + (col & 3)] = acc[0][0][e];
+        }
+        __syncthreads();
+        return;
+    }
     const int r2 = lane >> 5, l32 = lane & 31;   // fetching lanes: two columns of w at a time, 32 vectors of a piece each
     constexpr int pstep = part_step(PARTS);
     const int xrow = SRC == 1 ? col & (pstep - 1) : col;
@@ -574,6 +608,7 @@ __global__ __launch_bounds__(MFMA_WAVES * 64) void k_linear_few_mfma(FewParams f
                 for (int q = 0; q < KS; ++q) o += p[q * 256 + tt + 128];
         }
         const int r = row_of(t), n = n0 + col_of(t);
+        if (LOW) o += rs[t];
         if (SRC == 1) {
             float m = 0.f;
             for (int q = 0; q < KS; ++q) m += ((const float*)(lds + q * 16 * WPITCH))[r];
@@ -603,23 +638,25 @@ __global__ __launch_bounds__(MFMA_WAVES * 64) void k_linear_few_mfma(FewParams f
     move_pieces(fo, nthr);
 }
 
-template <int SRC, bool STEP, int PARTS, bool STREAM, int PPW, bool TURNS>
+template <int SRC, bool STEP, int PARTS, bool STREAM, int PPW, bool TURNS, bool LOW = false>
 hipError_t launch_few_mfma_kernel(const FewParams& fp, const FewOperands& fo, int wgs, size_t lds, hipStream_t st) {
     static bool raised[64];  // per device: more dynamic LDS than the default limit
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
     if (!raised[dev]) {
-        const hipError_t e = hipFuncSetAttribute((const void*)k_linear_few_mfma<SRC, STEP, PARTS, STREAM, PPW, TURNS>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)few_mfma_lds(MFMA_WAVES, mfma_tiles(MFMA_WAVES)));
+        const hipError_t e = hipFuncSetAttribute((const void*)k_linear_few_mfma<SRC, STEP, PARTS, STREAM, PPW, TURNS, LOW>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)few_mfma_lds(MFMA_WAVES, mfma_tiles(MFMA_WAVES)) + (LOW ? mfma_tiles(1) * 1024 : 0));
         if (e != hipSuccess) return e;
         raised[dev] = true;
     }
-    hipLaunchKernelGGL((k_linear_few_mfma<SRC, STEP, PARTS, STREAM, PPW, TURNS>), dim3(wgs), dim3(fo.ks * 64), lds, st, fp, fo);
+    hipLaunchKernelGGL((k_linear_few_mfma<SRC, STEP, PARTS, STREAM, PPW, TURNS, LOW>), dim3(wgs), dim3((fo.ks + LOW) * 64), lds, st, fp, fo);
     return hipGetLastError();
 }
 
 template <int SRC, int PARTS, int PPW, bool TURNS>
 hipError_t launch_few_mfma_pieces(const FewParams& fp, const FewOperands& fo, int wgs, size_t lds, hipStream_t st) {
+    if constexpr (SRC == 0)
+        if (fo.low.up) return launch_few_mfma_kernel<SRC, false, PARTS, false, PPW, TURNS, true>(fp, fo, wgs, lds + (fo.cols + 15) / 16 * 1024, st);
     if (fo.stream)
         return fo.cs ? launch_few_mfma_kernel<SRC, true, PARTS, true, PPW, TURNS>(fp, fo, wgs, lds, st)
                      : launch_few_mfma_kernel<SRC, false, PARTS, true, PPW, TURNS>(fp, fo, wgs, lds, st);
@@ -657,14 +694,14 @@ hipError_t launch_few_mfma_src(const FewParams& fp, const FewOperands& fo, int p
 struct FewSplit {
     int ks, ppw, cols, wgs;
 };
-FewSplit few_split(int K, int N, bool two, bool whole, int lone) {  // two pieces a wave where one is not enough; whole tiles; rows of a product alone (else 0)
+FewSplit few_split(int K, int N, bool two, bool whole, int lone, int most) {  // two pieces a wave where one is not enough; whole tiles; rows of a product alone (else 0); waves
     FewSplit f;
     const int pieces = (K + PIECE - 1) / PIECE;
     const bool longer = (lone <= 4 || K % 2048 == 0) && (N >= 32768 || (int64_t)N * K >= 1 << 27), single = lone && lone <= 8 && pieces > 1 && (pieces <= 4 || longer);
-    f.ppw = two && !single && (pieces > MFMA_WAVES || (pieces > 10 && N > 256 * 64)) ? 2 : 1;  // (twelve waves have four tiles: one round, or six waves with six)
+    f.ppw = two && !single && (pieces > most || (pieces > 10 && N > 256 * 64)) ? 2 : 1;  // (twelve waves have four tiles: one round, or six waves with six)
     const int need = (pieces + f.ppw - 1) / f.ppw;
     auto waves = [&](int turns) { return (need + turns - 1) / turns; };
-    int turns = single ? (need % 8 ? (need + 3) / 4 : need / 8) : need <= MFMA_WAVES ? 1 : (need + 9) / 10;
+    int turns = single ? (need % 8 ? (need + 3) / 4 : need / 8) : need <= most ? 1 : (need + 9) / 10;
     if (!single && turns > 1 && waves(turns + 1) > 5 && waves(turns + 1) * (turns + 1) < waves(turns) * turns) ++turns;
     f.ks = waves(turns);
     const int cols = even_columns(N, K, 256 * ((10 + f.ks / 2) / f.ks), 16 * mfma_tiles(f.ks));
@@ -675,7 +712,7 @@ FewSplit few_split(int K, int N, bool two, bool whole, int lone) {  // two piece
 }
 
 hipError_t launch_few_mfma(const FewParams& fp, FewOperands fo, int src, hipStream_t st) {
-    const FewSplit f = few_split(fp.K, fp.N, src != 1, fo.pack_out != nullptr, src == 0 && !fo.cs ? fp.rows : 0);
+    const FewSplit f = few_split(fp.K, fp.N, src != 1, fo.pack_out != nullptr, src == 0 && !fo.cs ? fp.rows : 0, fo.low.up ? MFMA_WAVES - 1 : MFMA_WAVES);
     const int ppw = f.ppw, wgs = f.wgs;
     const size_t lds = few_mfma_lds(f.ks, (f.cols + 15) / 16);
     fo.ks = f.ks;
@@ -926,6 +963,7 @@ bool few_rows_supported(const FewRowsJob& j) {
         if (j.pack_out && (!j.pack_ssq || !al16(j.pack_out))) return false;
     }
     if (j.mode == 1 && (!j.in_w || !al16(j.in_w))) return false;
+    if (j.low && (j.mode || j.cs || j.res || j.copy_bytes || j.pack_out || j.stream)) return false;  // a product alone
     if (j.res && j.ldres < j.N) return false;
     if (j.copy_bytes) {
         const size_t chunks = j.copy_chunks > 0 ? j.copy_chunks : 1;
@@ -965,6 +1003,8 @@ hipError_t launch_linear_few_rows(const FewRowsJob& j, hipStream_t st) {
     fo.pack_w = j.pack_w;
     fo.pack_ssq = j.pack_ssq;
     fo.stream = j.stream;
+    if (j.low) fo.low = *j.low;
+    else fo.low.up = nullptr;
     fo.cs = (__bf16*)j.cs;
     fo.cs_bs = j.cs_bs;
     fo.conv_w = j.conv_w;

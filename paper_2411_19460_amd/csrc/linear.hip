@@ -637,6 +637,20 @@ hipError_t launch_low_mixed(GemmParams gp, int n1, const LowRankTerm& lr, hipStr
     return hipGetLastError();
 }
 
+FewRowsJob few_rows_job(const GemmParams& gp) {  // a token or a few: bound by reading w once, not by the matrix cores
+    FewRowsJob j;
+    memset(&j, 0, sizeof(j));
+    j.rows = gp.M;
+    j.K = gp.K;
+    j.N = gp.N;
+    j.x = gp.A;
+    j.ldx = gp.lda;
+    j.w = gp.B;
+    j.out = gp.C;
+    j.ldo = gp.ldc;
+    return j;
+}
+
 }  // namespace
 
 int linear_check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ldo) { return check(rows, in_dim, out_dim, ldx, ldo); }
@@ -660,6 +674,11 @@ hipError_t launch_linear_low(bool input_grad, int64_t rows, int in_dim, int out_
         backward_widths(&gp, nullptr, wx, ww, first);
         return wx == 4 ? launch_low<false, 4>(gp, lr, st) : launch_low<false, 2>(gp, lr, st);
     }
+    if (rows <= FEW_ROWS) {
+        FewRowsJob j = few_rows_job(gp);
+        j.low = &lr;
+        if (few_rows_supported(j)) return launch_linear_few_rows(j, st);
+    }
     const ForwardPlan f = forward_plan(gp);
     if (f.n1 < gp.N) return f.w == 4 ? launch_low_mixed<4, 3>(gp, f.n1, lr, st) : launch_low_mixed<3, 2>(gp, f.n1, lr, st);
     return f.w == 4 ? launch_low<true, 4>(gp, lr, st) : f.w == 3 ? launch_low<true, 3>(gp, lr, st) : launch_low<true, 2>(gp, lr, st);
@@ -675,19 +694,6 @@ extern "C" int ssd_linear_fwd(int64_t rows, int32_t in_dim, int32_t out_dim, con
     if (rows == 0) return SSD_OK;
     if (!x || !w || !out) return SSD_ERR_NULL;
     if (!ok_ptr(x) || !ok_ptr(w) || !ok_ptr(out)) return SSD_ERR_ARG;
-    if (rows <= FEW_ROWS) {  // a token or a few: bound by reading w once, not by the matrix cores
-        FewRowsJob j;
-        memset(&j, 0, sizeof(j));
-        j.rows = (int)rows;
-        j.K = in_dim;
-        j.N = out_dim;
-        j.x = x;
-        j.ldx = x_row_stride ? x_row_stride : in_dim;
-        j.w = w;
-        j.out = out;
-        j.ldo = out_row_stride ? out_row_stride : out_dim;
-        if (few_rows_supported(j)) return launch_linear_few_rows(j, (hipStream_t)hip_stream) == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
-    }
     GemmParams gp;
     memset(&gp, 0, sizeof(gp));
     gp.A = (const bf16_t*)x;   // [rows, in]   k-major
@@ -699,8 +705,12 @@ extern "C" int ssd_linear_fwd(int64_t rows, int32_t in_dim, int32_t out_dim, con
     gp.M = (int)rows;
     gp.N = out_dim;
     gp.K = in_dim;
-    const ForwardPlan f = forward_plan(gp);
     hipStream_t st = (hipStream_t)hip_stream;
+    if (rows <= FEW_ROWS) {
+        const FewRowsJob j = few_rows_job(gp);
+        if (few_rows_supported(j)) return launch_linear_few_rows(j, st) == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
+    }
+    const ForwardPlan f = forward_plan(gp);
     hipError_t e;
     if (f.n1 < gp.N) e = f.w == 4 ? launch_mixed<4, 3>(gp, f.n1, st) : launch_mixed<3, 2>(gp, f.n1, st);
     else e = f.w == 4 ? launch_big<4>(gp, st) : f.w == 3 ? launch_big<3>(gp, st) : launch_big<2>(gp, st);

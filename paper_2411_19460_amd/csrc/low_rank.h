@@ -9,8 +9,9 @@ namespace ssdk {
 // the plan (LOW_TILE).  Both operands have the rank contiguous, so a lane's eight values are one piece of memory and nothing goes
 // through LDS.  `low` is rounded to bf16: the result is, and the term is the smaller part of it.  A row keeps the products with its own
 // adapter alone, by a selection and not by zeros in `low`: an infinity in one adapter stays with the rows that have it.  Of the
-// tile's adapters this call takes numbers u0, u0 + ustep, ...
-template <int MT, int NT>
+// tile's adapters this call takes numbers u0, u0 + ustep, ..., UB of them at a time: with more than one all of their operands are asked
+// for before the first is used, and none is left out for having no row here.
+template <int MT, int NT, int UB = 1>
 static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], const LowRankTerm& lr, int m0, int M, int n0, int N, int lane, int u0, int ustep) {
     using namespace mf;
     const int tile = m0 / LOW_TILE, nu = lr.tile_n[tile], q = lane >> 4, l16 = lane & 15;
@@ -36,28 +37,35 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
                 for (int e = 0; e < 4; ++e) a[i][e] = (__bf16)p0[e], a[i][4 + e] = (__bf16)p1[e];
             }
         }
-        for (int u = u0; u < nu; u += ustep) {
-            const int ad = list[u];
-            bool any = false;
+        for (int u = u0; u < nu; u += UB * ustep) {
+            int ad[UB];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) any = any || of_row[i] == ad;
-            if (!__any(any)) continue;
-            const bf16_t* up = lr.up + (int64_t)ad * lr.rank * lr.width + k;
-            bf16x8 b[NT];
+            for (int v = 0; v < UB; ++v) ad[v] = u + v * ustep < nu ? list[u + v * ustep] : -2;
+            if (UB == 1) {
+                bool any = false;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int n = n0 + 16 * j + l16;
-                b[j] = (bf16x8)((__bf16)0.f);
-                if (in && n < N) b[j] = *(const bf16x8*)(up + (int64_t)n * lr.rank);
+                for (int i = 0; i < MT; ++i) any = any || of_row[i] == ad[0];
+                if (!__any(any)) continue;
             }
+            bf16x8 b[UB][NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+            for (int v = 0; v < UB; ++v)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], (f32x4)(0.f), 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] += of_row[i] == ad ? t[e] : 0.f;
+                for (int j = 0; j < NT; ++j) {
+                    const int n = n0 + 16 * j + l16;
+                    b[v][j] = (bf16x8)((__bf16)0.f);
+                    if (in && n < N && (UB == 1 || ad[v] >= 0)) b[v][j] = *(const bf16x8*)(lr.up + ((int64_t)ad[v] * lr.width + n) * lr.rank + k);
                 }
+#pragma unroll
+            for (int v = 0; v < UB; ++v)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[v][j], a[i], (f32x4)(0.f), 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] += of_row[i] == ad[v] ? t[e] : 0.f;
+                    }
         }
     }
 }

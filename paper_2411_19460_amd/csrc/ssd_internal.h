@@ -403,6 +403,7 @@ struct FewRowsJob {
     const float *conv_w, *conv_b, *dt_bias;
     int off_xbc, off_dt;
     bool stream;  // w by streaming loads: it will not be in a cache when it is read again
+    const LowRankTerm* low;  // mode 0 and nothing else: with this term (null: none); host pointer
 };
 bool few_rows_supported(const FewRowsJob& j);  // sizes, strides and 16-byte alignment the kernel relies on
 hipError_t launch_linear_few_rows(const FewRowsJob& j, hipStream_t st);
