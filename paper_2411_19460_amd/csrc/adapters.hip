@@ -7,6 +7,8 @@
 // h and g are fp32, and so is everything that is summed: the gradients leave in fp32, and would lose 16 of its bits with either in bf16.
 #include <string.h>
 
+#include <type_traits>
+
 #include "mfma_common.h"
 
 namespace ssdk {
@@ -203,58 +205,82 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* rows, i
         ur[t] = ua + (int64_t)(r < lp.rank ? r : lp.rank - 1) * lp.K;
     }
     char* mine = lds + w * 64 * low_pitch<RT>();
-    const int vpr = nr / 8;  // KROW: 16-byte pieces of a row of U
+    const int vpr = nr / 8;  // KROW: 16-byte pieces of a row of U; (row, piece) of this lane's
+    int kp[2 * RT], cp[2 * RT];
+#pragma unroll
+    for (int i = 0; i < 2 * RT; ++i) {
+        kp[i] = (i * 64 + lane) / vpr;
+        cp[i] = (i * 64 + lane) - kp[i] * vpr;
+    }
     f32x4 acc[RT][MT];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[t][i] = (f32x4)(0.f);
-    for (int k0 = 64 * w; k0 < lp.K; k0 += 64 * LWAVES) {
-        bf16x8 xv[MT][2], uv[RT][2];
+    // U steps at a time: all that they need is asked for before the first is used.  WHOLE: all of their k exist; else what lies beyond K
+    // comes from k = 0 and is put to zero (in both operands: an infinity there would be a NaN).
+    constexpr int U = RT == 4 ? 2 : 4;
+    auto steps = [&](int k0, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        bf16x8 xv[U][MT][2], uv[U][KROW ? 2 * RT : RT * 2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = k0 + 16 * q + 8 * h;
-            const bool in = k < lp.K;
+        for (int s = 0; s < U; ++s) {
+            const int ks = k0 + 64 * LWAVES * s;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                xv[i][h] = (bf16x8)((__bf16)0.f);
-                if (in) xv[i][h] = *(const bf16x8*)(xr[i] + k);
+            for (int h = 0; h < 2; ++h) {
+                const int k = ks + 16 * q + 8 * h, kc = WHOLE || k < lp.K ? k : 0;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) xv[s][i][h] = *(const bf16x8*)(xr[i] + kc);
+                if (!KROW)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) uv[s][2 * t + h] = *(const bf16x8*)(ur[t] + kc);
             }
-            if (!KROW)
+            if (KROW)
+#pragma unroll
+                for (int i = 0; i < 2 * RT; ++i) {
+                    const int k = ks + kp[i];
+                    uv[s][i] = *(const bf16x8*)(ua + (int64_t)(WHOLE || k < lp.K ? k : 0) * lp.rank + r0 + 8 * cp[i]);
+                }
+        }
+#pragma unroll
+        for (int s = 0; s < U; ++s) {
+            const int ks = k0 + 64 * LWAVES * s;
+            if (!WHOLE && ks >= lp.K) break;
+            bf16x8 uo[RT][2];
+            if (KROW) {  // the wave's own rows of LDS, whose operations are done in order
+#pragma unroll
+                for (int i = 0; i < 2 * RT; ++i)
+                    if (kp[i] < 64) *(bf16x8*)(mine + kp[i] * low_pitch<RT>() + 16 * cp[i]) = WHOLE || ks + kp[i] < lp.K ? uv[s][i] : (bf16x8)((__bf16)0.f);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const char* p = mine + (16 * q + 8 * h + (l16 >> 2)) * low_pitch<RT>() + 32 * t + 8 * (l16 & 3);
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * low_pitch<RT>()));
+                        uo[t][h] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool in = WHOLE || ks + 16 * q + 8 * h < lp.K;
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    if (!in) xv[s][i][h] = (bf16x8)((__bf16)0.f);
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
-                    uv[t][h] = (bf16x8)((__bf16)0.f);
-                    if (in) uv[t][h] = *(const bf16x8*)(ur[t] + k);
-                }
-        }
-        if (KROW) {
-            // the wave's own rows: LDS operations of a wave are done in order
+                    if (!KROW) uo[t][h] = in ? uv[s][2 * t + h] : (bf16x8)((__bf16)0.f);
 #pragma unroll
-            for (int i = 0; i < 2 * RT; ++i) {
-                const int v = i * 64 + lane, k = v / vpr, c = v - k * vpr;
-                bf16x8 b = (bf16x8)((__bf16)0.f);
-                if (k < 64 && k0 + k < lp.K) b = *(const bf16x8*)(ua + (int64_t)(k0 + k) * lp.rank + r0 + 8 * c);
-                if (k < 64) *(bf16x8*)(mine + k * low_pitch<RT>() + 16 * c) = b;
+                    for (int i = 0; i < MT; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uo[t][h], xv[s][i][h], acc[t][i], 0, 0, 0);
+                }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const char* p = mine + (16 * q + 8 * h + (l16 >> 2)) * low_pitch<RT>() + 32 * t + 8 * (l16 & 3);
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * low_pitch<RT>()));
-                    uv[t][h] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int i = 0; i < MT; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uv[t][h], xv[i][h], acc[t][i], 0, 0, 0);
-    }
+    };
+    int k0 = 64 * w;
+    for (; k0 + 64 * (LWAVES * (U - 1) + 1) <= lp.K; k0 += 64 * LWAVES * U) steps(k0, std::true_type{});
+    if (k0 < lp.K) steps(k0, std::false_type{});
     __syncthreads();
     // lane -> row l16 of the unit's tile i, four consecutive ranks
     float* sums = (float*)lds;

@@ -367,6 +367,7 @@ typedef float f32x4v __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ int64_t packed_at(int row, int k) { return ((int64_t)(k >> 3) * 16 + row) * 8 + (k & 7); }
 
 constexpr int PIECE = 256, WPITCH = PIECE * 2 + 16;  // k per piece; bytes per LDS row of a piece of w
+constexpr int LOW_WAVES = 2;  // for a low-rank term
 constexpr int MFMA_WAVES = 12, MFMA_COLS = 16, MAX_GROUPS = 8;  // waves of a workgroup at most, columns at least
 __host__ __device__ constexpr int mfma_tiles(int ks) { return ks > 10 ? 4 : 6; }  // tiles of 16 columns at most: LDS
 // Up to eight rows leave rows of a tile free: they carry what rounding the operand x in_w to bf16 left of the live rows, and
@@ -407,12 +408,15 @@ __global__ __launch_bounds__(MFMA_WAVES * 64) void k_linear_few_mfma(FewParams f
     float* part = (float*)(lds + KS * 16 * WPITCH);  // [tiles][KS][256]
     float* rs = part + tiles * KS * 256;             // [groups][16]: 1 / rms, or (one group) [16][17]: shares of the squares
     const int col = lane & 15, kq = lane >> 4;   // operand lanes: row of x / column of w, quarter of a 32-wide k step
-    if (LOW && wv == KS) {  // rs: [tiles][256], laid out as a wave's partial tile
-        for (int t = 0; t < tiles; ++t) {
-            mf::f32x4 acc[1][1] = {{(mf::f32x4)(0.f)}};
-            add_low_rank<1, 1, 8>(acc, fo.low, 0, fp.rows, n0 + 16 * t, n0 + ncols, lane, 0, 1);
+    if (LOW && wv >= KS) {  // rs: [tiles][256], laid out as a wave's partial tile; two tiles at a time, the waves in turn
+        for (int t = 2 * (wv - KS); t < tiles; t += 2 * LOW_WAVES) {
+            mf::f32x4 acc[1][2] = {{(mf::f32x4)(0.f), (mf::f32x4)(0.f)}};
+            add_low_rank<1, 2, 8>(acc, fo.low, 0, fp.rows, n0 + 16 * t, n0 + ncols, lane, 0, 1);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) rs[t * 256 + 4 * (4 * kq + e + 16 * (col >> 2)) + (col & 3)] = acc[0][0][e];
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t + j < tiles) rs[(t + j) * 256 + 4 * (4 * kq + e + 16 * (col >> 2)) + (col & 3)] = acc[0][j][e];
         }
         __syncthreads();
         return;
@@ -649,7 +653,7 @@ hipError_t launch_few_mfma_kernel(const FewParams& fp, const FewOperands& fo, in
         if (e != hipSuccess) return e;
         raised[dev] = true;
     }
-    hipLaunchKernelGGL((k_linear_few_mfma<SRC, STEP, PARTS, STREAM, PPW, TURNS, LOW>), dim3(wgs), dim3((fo.ks + LOW) * 64), lds, st, fp, fo);
+    hipLaunchKernelGGL((k_linear_few_mfma<SRC, STEP, PARTS, STREAM, PPW, TURNS, LOW>), dim3(wgs), dim3((fo.ks + (LOW ? LOW_WAVES : 0)) * 64), lds, st, fp, fo);
     return hipGetLastError();
 }
 
@@ -712,7 +716,7 @@ FewSplit few_split(int K, int N, bool two, bool whole, int lone, int most) {  //
 }
 
 hipError_t launch_few_mfma(const FewParams& fp, FewOperands fo, int src, hipStream_t st) {
-    const FewSplit f = few_split(fp.K, fp.N, src != 1, fo.pack_out != nullptr, src == 0 && !fo.cs ? fp.rows : 0, fo.low.up ? MFMA_WAVES - 1 : MFMA_WAVES);
+    const FewSplit f = few_split(fp.K, fp.N, src != 1, fo.pack_out != nullptr, src == 0 && !fo.cs ? fp.rows : 0, fo.low.up ? MFMA_WAVES - LOW_WAVES : MFMA_WAVES);
     const int ppw = f.ppw, wgs = f.wgs;
     const size_t lds = few_mfma_lds(f.ks, (f.cols + 15) / 16);
     fo.ks = f.ks;
