@@ -20,11 +20,16 @@ using namespace mf;
 // Rows in the order of their adapters (stable; rows without one last), cut into units of rows that share one: short units for the
 // narrow products, long ones for the gradients, where a unit is what is summed before anything leaves for memory.  And for every tile
 // of the wide product the adapters that its rows have.  Words of 32 bits; host and device derive the places from (rows, adapters).
-constexpr int SHORT_UNIT = 32, PLAN_HDR = 16, MAX_RANK = 256;
+constexpr int SHORT_UNIT = 32, MAX_RANK = 256;
 
+// A unit: rows perm[first .. first + count - 1] of an adapter (a == n: rows without one).  row0 >= 0: they are row0, row0 + 1, ...  One load
+// tells a workgroup all that it needs; units that a batch does not have are there with no rows.
+struct Unit {
+    int a, first, count, row0;
+};
 struct Plan {
     int rows, n, long_unit, max_short, max_long, tiles;
-    int64_t ids, perm, start, first_short, first_long, first_slot, short_a, long_a, tile_n, tile_a, counts, words;
+    int64_t ids, perm, start, first_long, first_slot, short_u, long_u, tile_n, tile_a, counts, words;
 };
 
 int long_unit_of(int64_t rows) {  // about sixteen units where all rows share an adapter
@@ -41,7 +46,7 @@ Plan plan_of(int64_t rows, int32_t n) {
     p.max_short = least(rows, rows / SHORT_UNIT + n + 1);
     p.max_long = least(rows, rows / p.long_unit + n);
     p.tiles = (int)((rows + LOW_TILE - 1) / LOW_TILE);
-    int64_t at = PLAN_HDR;
+    int64_t at = 0;
     auto take = [&](int64_t words) {
         const int64_t here = at;
         at += (words + 3) / 4 * 4;
@@ -50,11 +55,10 @@ Plan plan_of(int64_t rows, int32_t n) {
     p.ids = take(rows);
     p.perm = take(rows);
     p.start = take(n + 2);        // of adapter a in perm; [n]: of the rows without one
-    p.first_short = take(n + 2);
     p.first_long = take(n + 1);
     p.first_slot = take(n + 1);   // partial sums of the gradients: adapters of several long units
-    p.short_a = take(p.max_short);
-    p.long_a = take(p.max_long);
+    p.short_u = take(4 * (int64_t)p.max_short);
+    p.long_u = take(4 * (int64_t)p.max_long);
     p.tile_n = take(p.tiles);
     p.tile_a = take((int64_t)p.tiles * LOW_TILE);
     p.counts = take(n + 1);
@@ -133,22 +137,15 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
     const int mine = plan[p.counts + a], ns = shorts(mine), nl = longs(mine);
     if (tid == 0) {
         plan[p.start + a] = start;
-        plan[p.first_short + a] = fs;
-        if (a < p.n) {
-            plan[p.first_long + a] = fl;
-            plan[p.first_slot + a] = fp;
-        } else {
-            plan[p.start + a + 1] = start + mine;
-            plan[p.first_short + a + 1] = fs + ns;
-            plan[p.first_long + a] = fl;
-            plan[p.first_slot + a] = fp;
-            plan[0] = fs + ns;
-            plan[1] = fl;
-        }
+        plan[p.first_long + a] = fl;
+        plan[p.first_slot + a] = fp;
+        if (a == p.n) plan[p.start + a + 1] = start + mine;
     }
-    for (int u = tid; u < ns; u += PTHR) plan[p.short_a + fs + u] = a;
-    if (a < p.n)
-        for (int u = tid; u < nl; u += PTHR) plan[p.long_a + fl + u] = a;
+    Unit *su = (Unit*)(plan + p.short_u), *lu = (Unit*)(plan + p.long_u);
+    if (a == p.n) {
+        for (int u = fs + ns + tid; u < p.max_short; u += PTHR) su[u] = Unit{0, 0, 0, 0};
+        for (int u = fl + tid; u < p.max_long; u += PTHR) lu[u] = Unit{0, 0, 0, 0};
+    }
     int at = start;
     const int wanted = a < p.n ? a : -1;
     for (int64_t r0 = 0; r0 < p.rows && at < start + mine; r0 += PTHR) {
@@ -163,12 +160,24 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
         if (is) plan[p.perm + at + before + __popcll(m & ((1ull << lane) - 1))] = (int)r;
         at += lds[0] + lds[1] + lds[2] + lds[3];
     }
+    __syncthreads();  // the rows are in place (for this workgroup), the units can say whether theirs follow one another
+    const int* rows = plan + p.perm + start;
+    auto unit = [&](int u, int len) {
+        Unit t = {a, start + u * len, mine - u * len < len ? mine - u * len : len, rows[u * len]};
+        if (rows[u * len + t.count - 1] != t.row0 + t.count - 1) t.row0 = -1;  // (they ascend)
+        return t;
+    };
+    for (int u = tid; u < ns; u += PTHR) su[fs + u] = unit(u, SHORT_UNIT);
+    if (a < p.n)
+        for (int u = tid; u < nl; u += PTHR) lu[fl + u] = unit(u, p.long_unit);
 }
 
 // ---- the narrow products ----
 // low[t, r] = s_a sum_k X[t, k] U_a[r, k].  A workgroup takes a short unit and 16 RT of the ranks; its eight waves share out k in steps
-// of 64, of which a quarter wave takes sixteen consecutive k (32 bytes of a row at a lane), and their sums meet in LDS.  KROW: U is
-// stored with k as the row index ([K, rank], the output side of an adapter) and goes through LDS to be read transposed.
+// of 64 and their sums meet in LDS.  A step's rows come in as 128 contiguous bytes a row (eight rows an access) and are turned into
+// operands through LDS of the wave's own, without a barrier; fetched straight as operands (sixteen rows an access) the same loads took
+// 8192 x 2560 at rank 64 39 us.  KROW: U is stored with k as the row index ([K, rank], the output side of an adapter) and is read
+// transposed.
 struct LowParams {
     const __bf16* x;
     int64_t ldx;
@@ -179,32 +188,39 @@ struct LowParams {
 };
 constexpr int LWAVES = 8;
 
+constexpr int STEP_PITCH = 144;  // bytes of a row of a step in LDS: 64 k, and sixteen rows fall into distinct banks
 template <int RT>
 constexpr int low_pitch() { return 32 * RT + 16; }
 template <int RT, bool KROW>
+constexpr int low_tiles() { return SHORT_UNIT * STEP_PITCH + (KROW ? 64 * low_pitch<RT>() : 16 * RT * STEP_PITCH); }  // of a wave
+template <int RT, bool KROW>
 constexpr int low_lds() {
-    constexpr int tiles = KROW ? LWAVES * 64 * low_pitch<RT>() : 0, sums = LWAVES * SHORT_UNIT * 16 * RT * 4;
+    constexpr int tiles = LWAVES * low_tiles<RT, KROW>(), sums = LWAVES * SHORT_UNIT * 16 * RT * 4;
     return tiles > sums ? tiles : sums;
 }
 
 template <int RT, bool KROW, int MT>
-__device__ __forceinline__ void low_unit(const LowParams& lp, const int* rows, int cnt, int a, int r0, char* lds) {
+__device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, const Unit un, int r0, char* lds) {
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
     const int nr = lp.rank - r0 < 16 * RT ? lp.rank - r0 : 16 * RT;  // ranks of this workgroup
-    const __bf16* xr[MT];
+    const int cnt = un.count, a = un.a, r8 = lane >> 3, c8 = (lane & 7) * 8;  // fetching lanes: eight rows of 64 k
+    const __bf16* xr[2 * MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int r = i * 16 + l16;
-        xr[i] = lp.x + rows[r < cnt ? r : cnt - 1] * lp.ldx;
+    for (int i = 0; i < 2 * MT; ++i) {
+        const int r = i * 8 + r8 < cnt ? i * 8 + r8 : cnt - 1;
+        int64_t row = un.row0 + r;
+        if (un.row0 < 0) row = perm[un.first + r];
+        xr[i] = lp.x + row * lp.ldx + c8;
     }
     const __bf16* ua = lp.u + (int64_t)a * lp.rank * lp.K;
-    const __bf16* ur[RT];  // KROW: not used
+    const __bf16* ur[2 * RT];  // KROW: not used
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int r = r0 + 16 * t + l16;
-        ur[t] = ua + (int64_t)(r < lp.rank ? r : lp.rank - 1) * lp.K;
+    for (int t = 0; t < 2 * RT; ++t) {
+        const int r = r0 + 8 * t + r8;
+        ur[t] = ua + (int64_t)(r < lp.rank ? r : lp.rank - 1) * lp.K + c8;
     }
-    char* mine = lds + w * 64 * low_pitch<RT>();
+    char *mx = lds + w * low_tiles<RT, KROW>(), *mu = mx + SHORT_UNIT * STEP_PITCH;
+    const float s = lp.scale[a];
     const int vpr = nr / 8;  // KROW: 16-byte pieces of a row of U; (row, piece) of this lane's
     int kp[2 * RT], cp[2 * RT];
 #pragma unroll
@@ -220,62 +236,61 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* rows, i
     // U steps at a time: all that they need is asked for before the first is used.  WHOLE: all of their k exist; else what lies beyond K
     // comes from k = 0 and is put to zero (in both operands: an infinity there would be a NaN).
     constexpr int U = RT == 4 ? 2 : 4;
+    const bf16x8 zero = (bf16x8)((__bf16)0.f);
     auto steps = [&](int k0, auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
-        bf16x8 xv[U][MT][2], uv[U][KROW ? 2 * RT : RT * 2];
+        bf16x8 xv[U][2 * MT], uv[U][2 * RT];
 #pragma unroll
         for (int s = 0; s < U; ++s) {
-            const int ks = k0 + 64 * LWAVES * s;
+            const int ks = k0 + 64 * LWAVES * s, kc = WHOLE || ks + c8 < lp.K ? ks : -c8;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = ks + 16 * q + 8 * h, kc = WHOLE || k < lp.K ? k : 0;
+            for (int i = 0; i < 2 * MT; ++i) xv[s][i] = *(const bf16x8*)(xr[i] + kc);
 #pragma unroll
-                for (int i = 0; i < MT; ++i) xv[s][i][h] = *(const bf16x8*)(xr[i] + kc);
-                if (!KROW)
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) uv[s][2 * t + h] = *(const bf16x8*)(ur[t] + kc);
-            }
-            if (KROW)
-#pragma unroll
-                for (int i = 0; i < 2 * RT; ++i) {
+            for (int i = 0; i < 2 * RT; ++i) {
+                if (KROW) {
                     const int k = ks + kp[i];
                     uv[s][i] = *(const bf16x8*)(ua + (int64_t)(WHOLE || k < lp.K ? k : 0) * lp.rank + r0 + 8 * cp[i]);
+                } else {
+                    uv[s][i] = *(const bf16x8*)(ur[i] + kc);
                 }
+            }
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int s = 0; s < U; ++s) {
             const int ks = k0 + 64 * LWAVES * s;
             if (!WHOLE && ks >= lp.K) break;
-            bf16x8 uo[RT][2];
-            if (KROW) {  // the wave's own rows of LDS, whose operations are done in order
+            const bool in = WHOLE || ks + c8 < lp.K;
 #pragma unroll
-                for (int i = 0; i < 2 * RT; ++i)
-                    if (kp[i] < 64) *(bf16x8*)(mine + kp[i] * low_pitch<RT>() + 16 * cp[i]) = WHOLE || ks + kp[i] < lp.K ? uv[s][i] : (bf16x8)((__bf16)0.f);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            for (int i = 0; i < 2 * MT; ++i) *(bf16x8*)(mx + (i * 8 + r8) * STEP_PITCH + 2 * c8) = in ? xv[s][i] : zero;
+#pragma unroll
+            for (int i = 0; i < 2 * RT; ++i) {
+                if (!KROW) *(bf16x8*)(mu + (i * 8 + r8) * STEP_PITCH + 2 * c8) = in ? uv[s][i] : zero;
+                else if (kp[i] < 64) *(bf16x8*)(mu + kp[i] * low_pitch<RT>() + 16 * cp[i]) = WHOLE || ks + kp[i] < lp.K ? uv[s][i] : zero;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own rows: its LDS operations are done in order
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8 xo[MT], uo[RT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) xo[i] = *(const bf16x8*)(mx + (i * 16 + l16) * STEP_PITCH + 64 * h + 16 * q);
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    if (KROW) {
+                        const char* p = mu + (32 * h + 8 * q + (l16 >> 2)) * low_pitch<RT>() + 32 * t + 8 * (l16 & 3);
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * low_pitch<RT>()));
+                        uo[t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    } else {
+                        uo[t] = *(const bf16x8*)(mu + (t * 16 + l16) * STEP_PITCH + 64 * h + 16 * q);
+                    }
+                }
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const char* p = mine + (16 * q + 8 * h + (l16 >> 2)) * low_pitch<RT>() + 32 * t + 8 * (l16 & 3);
-                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * low_pitch<RT>()));
-                        uo[t][h] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                    }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    for (int i = 0; i < MT; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uo[t], xo[i], acc[t][i], 0, 0, 0);
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bool in = WHOLE || ks + 16 * q + 8 * h < lp.K;
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-                    if (!in) xv[s][i][h] = (bf16x8)((__bf16)0.f);
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    if (!KROW) uo[t][h] = in ? uv[s][2 * t + h] : (bf16x8)((__bf16)0.f);
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(uo[t][h], xv[s][i][h], acc[t][i], 0, 0, 0);
-                }
-            }
+            asm volatile("" ::: "memory");  // the next step's rows come in behind these reads
         }
     };
     int k0 = 64 * w;
@@ -289,14 +304,14 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* rows, i
 #pragma unroll
         for (int i = 0; i < MT; ++i) *(f32x4*)(sums + (w * SHORT_UNIT + i * 16 + l16) * 16 * RT + 16 * t + 4 * q) = acc[t][i];
     __syncthreads();
-    const float s = lp.scale[a];
     for (int v = tid; v < MT * 16 * 4 * RT; v += 64 * LWAVES) {
-        const int row = v / (4 * RT), c = 4 * (v - row * 4 * RT);
-        if (row >= cnt || c >= nr) continue;
+        const int r = v / (4 * RT), c = 4 * (v - r * 4 * RT);
+        if (r >= cnt || c >= nr) continue;
         f32x4 o = (f32x4)(0.f);
 #pragma unroll
-        for (int u = 0; u < LWAVES; ++u) o += *(const f32x4*)(sums + (u * SHORT_UNIT + row) * 16 * RT + c);
-        *(f32x4*)(lp.low + (int64_t)rows[row] * lp.rank + r0 + c) = o * s;
+        for (int u = 0; u < LWAVES; ++u) o += *(const f32x4*)(sums + (u * SHORT_UNIT + r) * 16 * RT + c);
+        const int64_t at = un.row0 < 0 ? perm[un.first + r] : un.row0 + r;
+        *(f32x4*)(lp.low + at * lp.rank + r0 + c) = o * s;
     }
 }
 
@@ -326,17 +341,20 @@ __global__ __launch_bounds__(64 * LWAVES) void k_low(LowParams lp, Plan p, const
         return;
     }
     const int u = blockIdx.x - (KROW ? tj.blocks : 0);
-    if (u >= plan[0]) return;
-    const int a = plan[p.short_a + u], first = plan[p.start + a] + SHORT_UNIT * (u - plan[p.first_short + a]);
-    const int left = plan[p.start + a + 1] - first, cnt = left < SHORT_UNIT ? left : SHORT_UNIT, r0 = blockIdx.y * 16 * RT;
-    const int* rows = plan + p.perm + first;
-    if (a == p.n) {  // rows without an adapter
+    const Unit un = ((const Unit*)(plan + p.short_u))[u];
+    const int r0 = blockIdx.y * 16 * RT;
+    const int* perm = plan + p.perm;
+    if (un.count == 0) return;
+    if (un.a == p.n) {  // rows without an adapter
         const int nr = lp.rank - r0 < 16 * RT ? lp.rank - r0 : 16 * RT;
-        for (int v = threadIdx.x; v < cnt * nr; v += 64 * LWAVES) lp.low[(int64_t)rows[v / nr] * lp.rank + r0 + v % nr] = 0.f;
+        for (int v = threadIdx.x; v < un.count * nr; v += 64 * LWAVES) {
+            const int64_t row = un.row0 < 0 ? perm[un.first + v / nr] : un.row0 + v / nr;
+            lp.low[row * lp.rank + r0 + v % nr] = 0.f;
+        }
         return;
     }
-    if (cnt <= 16) low_unit<RT, KROW, 1>(lp, rows, cnt, a, r0, low_lds_mem);
-    else low_unit<RT, KROW, 2>(lp, rows, cnt, a, r0, low_lds_mem);
+    if (un.count <= 16) low_unit<RT, KROW, 1>(lp, perm, un, r0, low_lds_mem);
+    else low_unit<RT, KROW, 2>(lp, perm, un, r0, low_lds_mem);
 }
 
 template <int RT, bool KROW>
@@ -384,11 +402,11 @@ struct GradParams {
 constexpr int GCOLS = 128, GRANKS = 64, GXP = GCOLS * 2 + 16, GSP = GRANKS * 2 + 16;
 
 template <int RT, bool TRANS>
-__device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& gp, const Plan& p, const int* plan, int u, int cb, int r0, char* lds) {
+__device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& gp, const Plan& p, const int* plan, const Unit un, int u, int cb, int r0, char* lds) {
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
-    const int a = plan[p.long_a + u], fl = plan[p.first_long + a], nl = plan[p.first_long + a + 1] - fl;
-    const int first = plan[p.start + a] + p.long_unit * (u - fl), left = plan[p.start + a + 1] - first, cnt = left < p.long_unit ? left : p.long_unit;
-    const int* rows = plan + p.perm + first;
+    const int a = un.a, cnt = un.count, fl = plan[p.first_long + a], nl = plan[p.first_long + a + 1] - fl;
+    const int* perm = plan + p.perm + un.first;
+    auto row = [&](int t) -> int64_t { return un.row0 < 0 ? perm[t] : un.row0 + t; };
     const int c0 = cb * GCOLS;
     char *lx = lds, *ls = lds + 64 * GXP;
     f32x4 acc[RT][2];
@@ -402,14 +420,14 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
         for (int i = 0; i < 4; ++i) {  // 64 rows of 16 pieces
             const int v = i * 256 + tid, t = v >> 4, c = (v & 15) * 8;
             xv[i] = (bf16x8)((__bf16)0.f);
-            if (t0 + t < cnt && c0 + c < jb.cols) xv[i] = *(const bf16x8*)(jb.x + rows[t0 + t] * jb.ldx + c0 + c);
+            if (t0 + t < cnt && c0 + c < jb.cols) xv[i] = *(const bf16x8*)(jb.x + row(t0 + t) * jb.ldx + c0 + c);
         }
         f32x4 sv[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) {  // 64 rows of 4 RT pieces of four ranks
             const int v = i * 256 + tid, t = v / (4 * RT), r = 4 * (v % (4 * RT));
             sv[i] = (f32x4)(0.f);
-            if (t0 + t < cnt && r0 + r < gp.rank) sv[i] = *(const f32x4*)(jb.s + (int64_t)rows[t0 + t] * gp.rank + r0 + r);
+            if (t0 + t < cnt && r0 + r < gp.rank) sv[i] = *(const f32x4*)(jb.s + row(t0 + t) * gp.rank + r0 + r);
         }
         __syncthreads();  // the operands before these have been read
 #pragma unroll
@@ -474,10 +492,11 @@ template <int RT>
 __global__ __launch_bounds__(256) void k_adapter_grads(GradParams gp, Plan p, const int* plan) {
     __shared__ __attribute__((aligned(16))) char lds[64 * GXP + 3 * 64 * GSP];
     const int u = blockIdx.y;
-    if (u >= plan[1]) return;
+    const Unit un = ((const Unit*)(plan + p.long_u))[u];
+    if (un.count == 0) return;
     const int b = blockIdx.x, r0 = blockIdx.z * 16 * RT;
-    if (b < gp.job[0].blocks) grad_unit<RT, false>(gp.job[0], gp, p, plan, u, b, r0, lds);
-    else grad_unit<RT, true>(gp.job[1], gp, p, plan, u, b - gp.job[0].blocks, r0, lds);
+    if (b < gp.job[0].blocks) grad_unit<RT, false>(gp.job[0], gp, p, plan, un, u, b, r0, lds);
+    else grad_unit<RT, true>(gp.job[1], gp, p, plan, un, u, b - gp.job[0].blocks, r0, lds);
 }
 
 // Adapters of several units: their sums in order; adapters without a row: zeros.
