@@ -296,7 +296,7 @@ int ssd_linear_bwd(int64_t rows, int32_t in_dim, int32_t out_dim, const void* x,
  *   plan   what ssd_adapter_plan leaves for a batch: the rows in the order of their adapters.  It depends on row_adapter alone and
  *          serves every projection of every layer, any number of calls, until the batch changes.  row_adapter [rows] int32 in any
  *          order; whatever lies outside 0 .. nadapters - 1 means no adapter.  rows and nadapters of a call must be the plan's.
- *   workspace: ssd_adapter_workspace_bytes bytes, 256-byte aligned (the forward call needs none where hidden is given)
+ *   workspace: ssd_adapter_workspace_bytes bytes, 256-byte aligned
  * rank: a multiple of 8 up to 256 (pad smaller ones with zeros: their gradients stay zero).  in_dim, out_dim and strides: multiples
  * of 8; pointers 16-byte aligned, the plan 256.  rows == 0: nothing but zeroed gradients.  Outputs must not overlap inputs or each
  * other.  Everything is enqueued on hip_stream; nothing is allocated.

@@ -608,10 +608,10 @@ def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False,
         hidden = torch.empty((rows, shape.rank), dtype=torch.float32, device=x.device)
     if hidden is not None:
         _check_hidden(hidden, rows, shape.rank)
-    elif workspace is None:
+    if workspace is None:
         workspace = _workspace(int(lib().ssd_adapter_workspace_bytes(ctypes.byref(shape), 0)), x.device)
     rc = lib().ssd_adapter_linear_fwd(ctypes.byref(shape), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(out),
-                                      _ptr(hidden), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(x))
+                                      _ptr(hidden), _ptr(workspace), workspace.numel(), _stream(x))
     if rc != 0:
         raise SSDError(rc, "ssd_adapter_linear_fwd")
     return {"out": out, "hidden": hidden}

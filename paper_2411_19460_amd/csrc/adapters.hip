@@ -532,6 +532,16 @@ size_t low_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->rows * s-
 size_t turned_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->nadapters * s->rank * s->in_dim * 2); }
 size_t part_bytes(const Plan& p, const ssd_adapter_shape_t* s, int cols) { return pad((size_t)most_slots(p) * s->rank * cols * sizeof(float)); }
 
+LowProduct product_of(const ssd_adapter_shape_t* s, bool input_grad, const void* x, const void* w, void* out) {
+    const int64_t ldx = s->x_row_stride ? s->x_row_stride : s->in_dim, ldo = s->out_row_stride ? s->out_row_stride : s->out_dim;
+    if (input_grad) return {true, s->rows, s->in_dim, s->out_dim, x, ldo, w, out, s->dx_row_stride ? s->dx_row_stride : s->in_dim};
+    return {false, s->rows, s->in_dim, s->out_dim, x, ldx, w, out, ldo};
+}
+size_t slice_bytes(const ssd_adapter_shape_t* s, bool input_grad) {
+    if (!s->rows) return 0;
+    return pad(linear_low_bytes(product_of(s, input_grad, (const void*)256, (const void*)256, (void*)256)));
+}
+
 template <int RT>
 hipError_t launch_grads_rt(const GradParams& gp, const Plan& p, const int* plan, hipStream_t st) {
     hipLaunchKernelGGL((k_adapter_grads<RT>), dim3(gp.job[0].blocks + gp.job[1].blocks, p.max_long, (gp.rank + 16 * RT - 1) / (16 * RT)), dim3(256), 0, st, gp, p, plan);
@@ -563,9 +573,10 @@ extern "C" int ssd_adapter_plan(int64_t rows, int32_t nadapters, const int32_t* 
 
 extern "C" size_t ssd_adapter_workspace_bytes(const ssd_adapter_shape_t* shape, int32_t is_backward) {
     if (check_shape(shape) != SSD_OK || shape->rows > SSD_MAX_ADAPTER_ROWS) return 0;
-    if (!is_backward) return low_bytes(shape) + 256;
+    if (!is_backward) return low_bytes(shape) + slice_bytes(shape, false) + 256;
     const Plan p = plan_of(shape->rows, shape->nadapters);
-    return 2 * low_bytes(shape) + turned_bytes(shape) + part_bytes(p, shape, shape->in_dim) + part_bytes(p, shape, shape->out_dim) + 256;
+    const size_t slices = slice_bytes(shape, true), parts = part_bytes(p, shape, shape->in_dim) + part_bytes(p, shape, shape->out_dim);
+    return 2 * low_bytes(shape) + turned_bytes(shape) + (slices > parts ? slices : parts) + 256;  // (one is read before the other is written)
 }
 
 extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const void* x, const void* w, const void* a, const void* b,
@@ -577,7 +588,7 @@ extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const vo
     if (shape->rows == 0) return SSD_OK;
     if (!x || !w || !a || !b || !scale || !plan || !out) return SSD_ERR_NULL;
     if (!al(x, 16) || !al(w, 16) || !al(a, 16) || !al(b, 16) || !al(out, 16) || !al(scale, 4) || !al(hidden, 16) || !al(plan, 256)) return SSD_ERR_ARG;
-    if (!hidden && (!workspace || !al(workspace, 256) || workspace_bytes < ssd_adapter_workspace_bytes(shape, 0))) return SSD_ERR_WORKSPACE;
+    if (!workspace || !al(workspace, 256) || workspace_bytes < ssd_adapter_workspace_bytes(shape, 0)) return SSD_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)hip_stream;
     const Plan p = plan_of(shape->rows, shape->nadapters);
     const int* pl = (const int*)plan;
@@ -586,8 +597,7 @@ extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const vo
     const LowParams lp = {(const __bf16*)x, ldx, (const __bf16*)a, scale, low, shape->in_dim, shape->rank};
     if (launch_low_products<false>(lp, p, pl, TurnJob{}, st) != hipSuccess) return SSD_ERR_LAUNCH;
     const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, low, (const bf16_t*)b, shape->rank, shape->out_dim};
-    const hipError_t e = launch_linear_low(false, shape->rows, shape->in_dim, shape->out_dim, x, ldx, w, out,
-                                           shape->out_row_stride ? shape->out_row_stride : shape->out_dim, lr, st);
+    const hipError_t e = launch_linear_low(product_of(shape, false, x, w, out), lr, (char*)workspace + low_bytes(shape), st);
     return e == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
 }
 
@@ -624,8 +634,7 @@ extern "C" int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const vo
     if (launch_low_products<true>(lg, p, pl, tj, st) != hipSuccess) return SSD_ERR_LAUNCH;
     if (dx) {
         const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, g, (const bf16_t*)turned, shape->rank, shape->in_dim};
-        if (launch_linear_low(true, shape->rows, shape->in_dim, shape->out_dim, dout, ldd, w, dx, shape->dx_row_stride ? shape->dx_row_stride : shape->in_dim, lr, st) != hipSuccess)
-            return SSD_ERR_LAUNCH;
+        if (launch_linear_low(product_of(shape, true, dout, w, dx), lr, part_a, st) != hipSuccess) return SSD_ERR_LAUNCH;
     }
     if (!da) return SSD_OK;
     if (!hidden) {

@@ -468,6 +468,41 @@ __global__ __launch_bounds__(GTHR, 1) void k_gemm_low_mixed(GemmParams p1, GemmP
     else gemm_tile<true, true, W2, true>(p2, blockIdx.x - first, &lr2);
 }
 
+// K in `slices` pieces of k_slice: slice s of a tile leaves its sums in fp32 at part + s M N (the low-rank term with the first).
+template <bool BK, int WJ>
+__global__ __launch_bounds__(GTHR, 1) void k_gemm_low_slices(GemmParams gp, LowRankTerm lr, int k_slice) {
+    const int nt = gp.tiles_m * gp.tiles_n, s = blockIdx.x / nt, k0 = s * k_slice;
+    gp.A += k0;
+    gp.B += BK ? (int64_t)k0 : (int64_t)k0 * gp.ldb;
+    gp.K = gp.K - k0 < k_slice ? gp.K - k0 : k_slice;
+    gp.C = (float*)gp.C + (int64_t)s * gp.M * gp.N;
+    if (s == 0) gemm_tile<true, BK, WJ, true>(gp, blockIdx.x, &lr);
+    else gemm_tile<true, BK, WJ>(gp, blockIdx.x - s * nt);
+}
+
+// out = the sum of the slices, in order, rounded once.
+__global__ __launch_bounds__(256) void k_sum_slices(const float* part, int slices, int M, int N, bf16_t* out, int64_t ldo) {
+    const int64_t size = (int64_t)M * N, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= size) return;
+    f32x4 o0 = (f32x4)(0.f), o1 = (f32x4)(0.f);
+    int s = 0;
+    for (; s + 4 <= slices; s += 4) {
+        f32x4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = *(const f32x4*)(part + (s + u / 2) * size + i + 4 * (u & 1));
+#pragma unroll
+        for (int u = 0; u < 8; u += 2) o0 += v[u], o1 += v[u + 1];
+    }
+    for (; s < slices; ++s) {
+        o0 += *(const f32x4*)(part + s * size + i);
+        o1 += *(const f32x4*)(part + s * size + i + 4);
+    }
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (__bf16)o0[e], o[4 + e] = (__bf16)o1[e];
+    *(bf16x8*)((__bf16*)out + i / N * ldo + i % N) = o;
+}
+
 bool ok_ptr(const void* p) { return p && ((uintptr_t)p & 15) == 0; }
 
 template <bool AK, bool BK, int WJ>
@@ -637,6 +672,24 @@ hipError_t launch_low_mixed(GemmParams gp, int n1, const LowRankTerm& lr, hipStr
     return hipGetLastError();
 }
 
+template <bool BK, int WJ>
+hipError_t launch_low_slices(GemmParams gp, const LowRankTerm& lr, int slices, float* part, hipStream_t st) {
+    constexpr int LDS = big_lds<true, BK, WJ>();
+    static bool raised[64];
+    const hipError_t e = allow_lds((const void*)k_gemm_low_slices<BK, WJ>, LDS, raised);
+    if (e != hipSuccess) return e;
+    const int steps = (gp.K + BKK - 1) / BKK, k_slice = (steps + slices - 1) / slices * BKK;
+    slices = (gp.K + k_slice - 1) / k_slice;  // none of them empty
+    bf16_t* out = (bf16_t*)gp.C;
+    gp.C = part;
+    const int64_t ldo = gp.ldc;
+    gp.ldc = gp.N;
+    gp.c_f32 = 1;
+    hipLaunchKernelGGL((k_gemm_low_slices<BK, WJ>), dim3(set_tiles(gp, WJ) * slices), dim3(GTHR), LDS, st, gp, lr, k_slice);
+    hipLaunchKernelGGL(k_sum_slices, dim3((unsigned)(((int64_t)gp.M * gp.N / 8 + 255) / 256)), dim3(256), 0, st, part, slices, gp.M, gp.N, out, ldo);
+    return hipGetLastError();
+}
+
 FewRowsJob few_rows_job(const GemmParams& gp) {  // a token or a few: bound by reading w once, not by the matrix cores
     FewRowsJob j;
     memset(&j, 0, sizeof(j));
@@ -655,33 +708,98 @@ FewRowsJob few_rows_job(const GemmParams& gp) {  // a token or a few: bound by r
 
 int linear_check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ldo) { return check(rows, in_dim, out_dim, ldx, ldo); }
 
-hipError_t launch_linear_low(bool input_grad, int64_t rows, int in_dim, int out_dim, const void* x, int64_t ldx, const void* w, void* out, int64_t ldo,
-                             const LowRankTerm& lr, hipStream_t st) {
+namespace {
+
+GemmParams low_params(const LowProduct& j) {
     GemmParams gp;
     memset(&gp, 0, sizeof(gp));
-    gp.A = (const bf16_t*)x;
-    gp.B = (const bf16_t*)w;  // [out_dim, in_dim]: k-major for the forward product, k as the row index for the gradient
-    gp.C = out;
-    gp.lda = ldx;
-    gp.ldb = in_dim;
-    gp.ldc = ldo;
-    gp.M = (int)rows;
-    gp.N = input_grad ? in_dim : out_dim;
-    gp.K = input_grad ? out_dim : in_dim;
-    if (input_grad) {
+    gp.A = (const bf16_t*)j.x;
+    gp.B = (const bf16_t*)j.w;  // [out_dim, in_dim]: k-major for the forward product, k as the row index for the gradient
+    gp.C = j.out;
+    gp.lda = j.ldx;
+    gp.ldb = j.in_dim;
+    gp.ldc = j.ldo;
+    gp.M = (int)j.rows;
+    gp.N = j.input_grad ? j.in_dim : j.out_dim;
+    gp.K = j.input_grad ? j.out_dim : j.in_dim;
+    return gp;
+}
+
+// How a product with a low-rank term runs: few rows as products that stream w (few_rows.hip), some tens to hundreds in small tiles whose
+// waves share out K (split_rows.hip, 32 rows x 16 `width` columns), more in the tiles above, 64 `width` columns, K cut into `slices`
+// where the tiles alone would leave compute units idle.  By the estimated time, us: a tile's K step of 64 columns x 4, 3, 2 takes 1.06,
+// 0.88, 0.67 and what surrounds the steps 7; slices cost a launch more (4) and their sums' way out and back (6 TB/s); a round of small
+// tiles costs 1 to 2 and, for each k, 1.1, 1.8, 2.4 ns at 16, 32, 64 columns (w with k as the row index: 2.2, 2.6, 3.0).  Measured
+// over 17 ... 4096 rows of five pairs of widths from 768 to 10576, small tiles / slices / whole tiles, narrow products included: 64 rows
+// 5120 -> 2560 19 / 28 / 64 us, 100 rows 25 / 31 / 65, 256 rows 40 / 36 / 67, 1000 rows - / 51 / 68, 4096 rows - / 113 / 99; 64 rows
+// 2560 -> 10576 25 / 31 / 40, 256 rows 60 / 38 / 42; input gradient of 2560 -> 10576, 32 rows 38 / 34 / 116, 256 rows 84 / 52 / 141,
+// 1000 rows - / 85 / 145.
+struct LowRun {
+    enum { FEW, SMALL, TILES } kind;
+    int width, slices;
+};
+LowRun low_run(const GemmParams& gp, bool input_grad) {
+    if (!input_grad && gp.M <= FEW_ROWS && few_rows_supported(few_rows_job(gp))) return {LowRun::FEW, 0, 1};
+    constexpr double STEP[5] = {0, 0, 0.67, 0.88, 1.06}, ROUND[5] = {0, 1.2, 1.5, 0, 2.0};
+    constexpr double PER_K[2][5] = {{0, 0.0011, 0.0018, 0, 0.0024}, {0, 0.0022, 0.0026, 0, 0.0030}};
+    const int steps = (gp.K + BKK - 1) / BKK;
+    auto rounds = [](int64_t wgs) { return (double)((wgs + UNITS - 1) / UNITS); };
+    LowRun best = {LowRun::TILES, 0, 1};  // width 0: the rules of the plain products
+    double t = 1e30;
+    for (int w = 4; w >= 2; w -= input_grad ? 2 : 1) {
+        const int64_t tiles = tile_count(gp, w);
+        const double one = rounds(tiles) * (steps * STEP[w] + 7);
+        if (one < t) t = one, best = {LowRun::TILES, 0, 1};
+        for (int s = 2; s <= 16 && steps / s >= 4 && tiles * s <= 2 * UNITS; ++s) {
+            const double c = rounds(tiles * s) * ((steps + s - 1) / s * STEP[w] + 7) + 4 + (double)s * gp.M * gp.N * 8 / 6e6;
+            if (c < t) t = c, best = {LowRun::TILES, w, s};
+        }
+    }
+    for (int w = 1; w <= 4; w *= 2) {
+        const int64_t wgs = (int64_t)((gp.M + 31) / 32) * ((gp.N + 16 * w - 1) / (16 * w));
+        const double c = 2 + rounds(wgs) * (ROUND[w] + PER_K[input_grad][w] * gp.K);
+        if (c < t) t = c, best = {LowRun::SMALL, w, 1};
+    }
+    return best;
+}
+
+template <bool BK>
+hipError_t launch_low_tiles(const GemmParams& gp, const LowRankTerm& lr, const LowRun& r, void* part, hipStream_t st) {
+    if (r.slices > 1) {
+        if constexpr (BK)
+            if (r.width == 3) return launch_low_slices<BK, 3>(gp, lr, r.slices, (float*)part, st);
+        return r.width == 4 ? launch_low_slices<BK, 4>(gp, lr, r.slices, (float*)part, st) : launch_low_slices<BK, 2>(gp, lr, r.slices, (float*)part, st);
+    }
+    if constexpr (BK) {
+        const ForwardPlan f = forward_plan(gp);
+        if (f.n1 < gp.N) return f.w == 4 ? launch_low_mixed<4, 3>(gp, f.n1, lr, st) : launch_low_mixed<3, 2>(gp, f.n1, lr, st);
+        return f.w == 4 ? launch_low<BK, 4>(gp, lr, st) : f.w == 3 ? launch_low<BK, 3>(gp, lr, st) : launch_low<BK, 2>(gp, lr, st);
+    } else {
         int wx, ww;
         bool first;
         backward_widths(&gp, nullptr, wx, ww, first);
-        return wx == 4 ? launch_low<false, 4>(gp, lr, st) : launch_low<false, 2>(gp, lr, st);
+        return wx == 4 ? launch_low<BK, 4>(gp, lr, st) : launch_low<BK, 2>(gp, lr, st);
     }
-    if (rows <= FEW_ROWS) {
-        FewRowsJob j = few_rows_job(gp);
-        j.low = &lr;
-        if (few_rows_supported(j)) return launch_linear_few_rows(j, st);
+}
+
+}  // namespace
+
+size_t linear_low_bytes(const LowProduct& j) {
+    const GemmParams gp = low_params(j);
+    const LowRun r = low_run(gp, j.input_grad);
+    return r.slices > 1 ? (size_t)r.slices * gp.M * gp.N * sizeof(float) : 0;
+}
+
+hipError_t launch_linear_low(const LowProduct& j, const LowRankTerm& lr, void* part, hipStream_t st) {
+    const GemmParams gp = low_params(j);
+    const LowRun r = low_run(gp, j.input_grad);
+    if (r.kind == LowRun::FEW) {
+        FewRowsJob f = few_rows_job(gp);
+        f.low = &lr;
+        return launch_linear_few_rows(f, st);
     }
-    const ForwardPlan f = forward_plan(gp);
-    if (f.n1 < gp.N) return f.w == 4 ? launch_low_mixed<4, 3>(gp, f.n1, lr, st) : launch_low_mixed<3, 2>(gp, f.n1, lr, st);
-    return f.w == 4 ? launch_low<true, 4>(gp, lr, st) : f.w == 3 ? launch_low<true, 3>(gp, lr, st) : launch_low<true, 2>(gp, lr, st);
+    if (r.kind == LowRun::SMALL) return launch_split_rows(j.input_grad, gp.M, gp.K, gp.N, j.x, gp.lda, j.w, gp.ldb, j.out, gp.ldc, r.width, lr, st);
+    return j.input_grad ? launch_low_tiles<false>(gp, lr, r, part, st) : launch_low_tiles<true>(gp, lr, r, part, st);
 }
 }  // namespace ssdk
 

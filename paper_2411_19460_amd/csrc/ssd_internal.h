@@ -358,8 +358,21 @@ struct LowRankTerm {
     int rank, width;    // width: columns of the whole product
 };
 int linear_check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ldo);  // sizes and strides, as ssd_linear_fwd
-// out = x w^T + low up (rows of in_dim -> out_dim), or with input_grad out = x w + low up (rows of out_dim -> in_dim)
-hipError_t launch_linear_low(bool input_grad, int64_t rows, int in_dim, int out_dim, const void* x, int64_t ldx, const void* w, void* out, int64_t ldo,
+// out = x w^T + low up^T (rows of in_dim -> out_dim), or with input_grad out = x w + low up^T (rows of out_dim -> in_dim)
+struct LowProduct {
+    bool input_grad;
+    int64_t rows;
+    int in_dim, out_dim;
+    const void* x;
+    int64_t ldx;
+    const void* w;
+    void* out;
+    int64_t ldo;
+};
+size_t linear_low_bytes(const LowProduct& j);  // of `part` (x, w and out are not looked at but for whether they are null)
+hipError_t launch_linear_low(const LowProduct& j, const LowRankTerm& lr, void* part, hipStream_t st);
+// The same in tiles of 32 rows and 16 nt columns (nt 1, 2, 4; split_rows.hip), K and N of the product
+hipError_t launch_split_rows(bool input_grad, int rows, int K, int N, const void* x, int64_t ldx, const void* w, int64_t ldw, void* out, int64_t ldo, int nt,
                              const LowRankTerm& lr, hipStream_t st);
 
 // Generation (few_rows.hip): products and the block's middle steps for at most FEW_ROWS tokens, bf16 storage.
