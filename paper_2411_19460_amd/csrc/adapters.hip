@@ -414,21 +414,24 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[t][j] = (f32x4)(0.f);
-    for (int t0 = 0; t0 < cnt; t0 += 64) {
-        bf16x8 xv[4];
+    bf16x8 xv[4];
+    f32x4 sv[RT];
+    auto load = [&](int t0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // 64 rows of 16 pieces
             const int v = i * 256 + tid, t = v >> 4, c = (v & 15) * 8;
             xv[i] = (bf16x8)((__bf16)0.f);
             if (t0 + t < cnt && c0 + c < jb.cols) xv[i] = *(const bf16x8*)(jb.x + row(t0 + t) * jb.ldx + c0 + c);
         }
-        f32x4 sv[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) {  // 64 rows of 4 RT pieces of four ranks
             const int v = i * 256 + tid, t = v / (4 * RT), r = 4 * (v % (4 * RT));
             sv[i] = (f32x4)(0.f);
             if (t0 + t < cnt && r0 + r < gp.rank) sv[i] = *(const f32x4*)(jb.s + row(t0 + t) * gp.rank + r0 + r);
         }
+    };
+    load(0);
+    for (int t0 = 0; t0 < cnt; t0 += 64) {
         __syncthreads();  // the operands before these have been read
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -447,6 +450,7 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
             }
         }
         __syncthreads();
+        load(t0 + 64);  // the next rows come in while these are multiplied
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int k = 32 * h + 8 * q + (l16 >> 2);

@@ -746,15 +746,20 @@ LowRun low_run(const GemmParams& gp, bool input_grad) {
     auto rounds = [](int64_t wgs) { return (double)((wgs + UNITS - 1) / UNITS); };
     LowRun best = {LowRun::TILES, 0, 1};  // width 0: the rules of the plain products
     double t = 1e30;
-    for (int w = 4; w >= 2; w -= input_grad ? 2 : 1) {
+    const int dw = input_grad ? 2 : 1;
+    for (int w = 4; w >= 2; w -= dw) {
+        const double one = rounds(tile_count(gp, w)) * (steps * STEP[w] + 7);
+        if (one < t) t = one;
+    }
+    t *= 0.9;  // slices for a tenth at least
+    for (int w = 4; w >= 2; w -= dw) {
         const int64_t tiles = tile_count(gp, w);
-        const double one = rounds(tiles) * (steps * STEP[w] + 7);
-        if (one < t) t = one, best = {LowRun::TILES, 0, 1};
         for (int s = 2; s <= 16 && steps / s >= 4 && tiles * s <= 2 * UNITS; ++s) {
             const double c = rounds(tiles * s) * ((steps + s - 1) / s * STEP[w] + 7) + 4 + (double)s * gp.M * gp.N * 8 / 6e6;
             if (c < t) t = c, best = {LowRun::TILES, w, s};
         }
     }
+    if (best.slices == 1) t /= 0.9;
     for (int w = 1; w <= 4; w *= 2) {
         const int64_t wgs = (int64_t)((gp.M + 31) / 32) * ((gp.N + 16 * w - 1) / (16 * w));
         const double c = 2 + rounds(wgs) * (ROUND[w] + PER_K[input_grad][w] * gp.K);
