@@ -329,7 +329,8 @@ int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const void* x, cons
  *           in time (it holds their partial sums).
  *   ssd_grad_norm: sum_sq (one double, device) = S, in fp64, in a fixed order.  Gradients that lie on several devices: add up their S
  *           in front of ssd_grad_clip.
- *   ssd_grad_clip: scales by the factor of *sum_sq; norm (one float, device) = sqrt(S), or NULL.  A gradient that is its own result is
+ *   ssd_grad_clip: scales by the factor of *sum_sq, or (sum_sq NULL) of the plan's own S, worked out on the way; norm (one float,
+ *           device) = sqrt(S), or NULL.  A gradient that is its own result is
  *           left alone where the factor is 1.  Non-finite gradients act as the formula says: an infinite norm gives a factor of 0
  *           (and NaN where 0 meets an infinity), a NaN makes everything NaN; the norm tells a caller to drop the step.
  * max_norm >= 0, infinity for the norm alone.  Everything is enqueued on hip_stream, nothing is allocated, the host does not wait.

@@ -704,13 +704,12 @@ def _check_sum_sq(sum_sq, plan):
 
 def ssd_grad_clip(plan: GradPlan, max_norm: float, sum_sq=None):
     """Scales the plan's gradients by min(1, max_norm / (norm + 1e-6)) into its results and returns norm [1] fp32.  sum_sq: the sum of
-    squares that the norm is the root of (None: the plan's own, by ssd_grad_norm)."""
+    squares that the norm is the root of (None: the plan's own)."""
     import torch
     if not max_norm >= 0:
         raise ValueError("max_norm must not be negative")
-    if sum_sq is None:
-        sum_sq = ssd_grad_norm(plan)
-    _check_sum_sq(sum_sq, plan)
+    if sum_sq is not None:
+        _check_sum_sq(sum_sq, plan)
     norm = torch.empty(1, dtype=torch.float32, device=plan.buffer.device)
     rc = lib().ssd_grad_clip(_ptr(plan.buffer), plan.pieces, _ptr(sum_sq), max_norm, _ptr(norm), _stream(plan.buffer))
     if rc != 0:

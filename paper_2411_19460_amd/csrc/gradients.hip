@@ -11,12 +11,13 @@ namespace ssdk {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int64_t PIECE = 8192;  // elements: a multiple of 16-byte vectors, so that all pieces of a tensor are aligned as it is
-constexpr int THR = 256, MAX_WGS = 2048;
+constexpr int THR = 256, NORM_WGS = 1024, CLIP_WGS = 2048;
 
-// Device memory of a plan: the counter of finished workgroups, their sums of squares, then the pieces.
+// Device memory of a plan: the workgroups' sums of squares, then the pieces.
 struct Piece {
     const void* src;
     void* dst;
@@ -24,9 +25,7 @@ struct Piece {
     int pad[2];
 };
 struct Head {
-    unsigned int done;
-    unsigned int pad[63];
-    double part[MAX_WGS];
+    double part[NORM_WGS];
 };
 static_assert(sizeof(Piece) == 32 && sizeof(Head) % 256 == 0, "");
 
@@ -40,8 +39,7 @@ struct Tensors {
     int count;
 };
 
-__global__ __launch_bounds__(THR) void k_grad_pieces(Tensors t, Piece* pieces, Head* head) {
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) head->done = 0;
+__global__ __launch_bounds__(THR) void k_grad_pieces(Tensors t, Piece* pieces) {
     for (int i = blockIdx.y; i < t.count; i += gridDim.y) {
         const int64_t np = (t.numel[i] + PIECE - 1) / PIECE;
         for (int64_t k = (int64_t)blockIdx.x * THR + threadIdx.x; k < np; k += (int64_t)gridDim.x * THR) {
@@ -59,7 +57,7 @@ __global__ __launch_bounds__(THR) void k_grad_pieces(Tensors t, Piece* pieces, H
 
 __device__ __forceinline__ double square(float v) { return (double)v * (double)v; }
 
-__device__ __forceinline__ double block_total(double v, double* lds) {  // in thread 0
+__device__ __forceinline__ double block_total(double v, double* lds) {  // in every thread
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
@@ -67,85 +65,120 @@ __device__ __forceinline__ double block_total(double v, double* lds) {  // in th
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+// Sums of squares of a piece's elements that fall to this thread.  A whole piece's loads are all asked for before the first is used.
 template <bool BF16>
 __device__ __forceinline__ double piece_squares(const Piece& p) {
-    double s = 0.0;
-    constexpr int V = BF16 ? 8 : 4;
+    constexpr int V = BF16 ? 8 : 4, L = PIECE / (V * THR);
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    auto add = [&](u32x4 bits) {
+        if (BF16) {
+            const bf16x8 x = __builtin_bit_cast(bf16x8, bits);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e & 3] += square((float)x[e]);
+        } else {
+            const f32x4 x = __builtin_bit_cast(f32x4, bits);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += square(x[e]);
+        }
+    };
     int i0 = 0;
     if (p.kind & 4) {
-        const int nv = p.n / V;
-        for (int v = threadIdx.x; v < nv; v += THR) {
-            if (BF16) {
-                const bf16x8 x = ((const bf16x8*)p.src)[v];
+        const u32x4* src = (const u32x4*)p.src + threadIdx.x;
+        if (p.n == PIECE) {
+            u32x4 x[L];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s += square((float)x[e]);
-            } else {
-                const f32x4 x = ((const f32x4*)p.src)[v];
+            for (int l = 0; l < L; ++l) x[l] = src[l * THR];
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s += square(x[e]);
-            }
+            for (int l = 0; l < L; ++l) add(x[l]);
+            return (s[0] + s[1]) + (s[2] + s[3]);
         }
+        const int nv = p.n / V;
+        for (int v = threadIdx.x; v < nv; v += THR, src += THR) add(*src);
         i0 = nv * V;
     }
-    for (int i = i0 + threadIdx.x; i < p.n; i += THR) s += square(BF16 ? (float)((const __bf16*)p.src)[i] : ((const float*)p.src)[i]);
-    return s;
+    for (int i = i0 + threadIdx.x; i < p.n; i += THR) s[0] += square(BF16 ? (float)((const __bf16*)p.src)[i] : ((const float*)p.src)[i]);
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// The workgroup that finishes last adds up the sums of all: their order is that of the workgroups, whoever is last.
-__global__ __launch_bounds__(THR) void k_grad_norm(const Piece* pieces, int64_t count, Head* head, double* sum_sq) {
+// part[w] = what workgroup w finds in its pieces
+__global__ __launch_bounds__(THR) void k_grad_squares(const Piece* __restrict__ pieces, int64_t count, double* part) {
     __shared__ double lds[4];
-    __shared__ int last;
     double s = 0.0;
     for (int64_t k = blockIdx.x; k < count; k += gridDim.x) {
         const Piece p = pieces[k];
         s += p.kind & 1 ? piece_squares<true>(p) : piece_squares<false>(p);
     }
     s = block_total(s, lds);
-    if (threadIdx.x == 0) {
-        __hip_atomic_store(&head->part[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const unsigned int before = __hip_atomic_fetch_add(&head->done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        last = before == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    s = 0.0;
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += THR) s += __hip_atomic_load(&head->part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s = block_total(s, lds);
-    if (threadIdx.x == 0) {
-        *sum_sq = s;
-        head->done = 0;  // for the next call
-    }
+    if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+// The sum of the workgroups' sums, in a fixed order: every workgroup that asks gets the same.
+__device__ __forceinline__ double sum_parts(const double* part, int parts, double* lds) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += THR) s += part[i];
+    return block_total(s, lds);
+}
+
+__global__ __launch_bounds__(THR) void k_grad_sum(const double* part, int parts, double* sum_sq) {
+    __shared__ double lds[4];
+    const double s = sum_parts(part, parts, lds);
+    if (threadIdx.x == 0) *sum_sq = s;
 }
 
 template <bool FROM, bool TO>
 __device__ __forceinline__ void scale_piece(const Piece& p, float c) {
+    struct Eight {
+        u32x4 a, b;
+    };
+    auto load = [&](int v) {
+        Eight x;
+        if (FROM) {
+            x.a = ((const u32x4*)p.src)[v];
+        } else {
+            x.a = ((const u32x4*)p.src)[2 * v];
+            x.b = ((const u32x4*)p.src)[2 * v + 1];
+        }
+        return x;
+    };
+    auto store = [&](int v, const Eight& x) {
+        float f[8];
+        if (FROM) {
+            const bf16x8 h = __builtin_bit_cast(bf16x8, x.a);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = (float)h[e] * c;
+        } else {
+            const f32x4 lo = __builtin_bit_cast(f32x4, x.a), hi = __builtin_bit_cast(f32x4, x.b);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = lo[e] * c, f[4 + e] = hi[e] * c;
+        }
+        if (TO) {
+            bf16x8 o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = (__bf16)f[e];
+            ((bf16x8*)p.dst)[v] = o;
+        } else {
+            f32x4 lo, hi;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lo[e] = f[e], hi[e] = f[4 + e];
+            ((f32x4*)p.dst)[2 * v] = lo;
+            ((f32x4*)p.dst)[2 * v + 1] = hi;
+        }
+    };
     int i0 = 0;
     if (p.kind & 4) {
-        const int nv = p.n / 8;
-        for (int v = threadIdx.x; v < nv; v += THR) {
-            float f[8];
-            if (FROM) {
-                const bf16x8 x = ((const bf16x8*)p.src)[v];
+        constexpr int L = PIECE / (8 * THR);
+        if (p.n == PIECE) {
+            Eight x[L];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = (float)x[e];
-            } else {
-                const f32x4 x0 = ((const f32x4*)p.src)[2 * v], x1 = ((const f32x4*)p.src)[2 * v + 1];
+            for (int l = 0; l < L; ++l) x[l] = load(l * THR + threadIdx.x);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = x0[e], f[4 + e] = x1[e];
-            }
-            if (TO) {
-                bf16x8 o;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = (__bf16)(f[e] * c);
-                ((bf16x8*)p.dst)[v] = o;
-            } else {
-                f32x4 o0, o1;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o0[e] = f[e] * c, o1[e] = f[4 + e] * c;
-                ((f32x4*)p.dst)[2 * v] = o0;
-                ((f32x4*)p.dst)[2 * v + 1] = o1;
-            }
+            for (int l = 0; l < L; ++l) store(l * THR + threadIdx.x, x[l]);
+            return;
         }
+        const int nv = p.n / 8;
+        for (int v = threadIdx.x; v < nv; v += THR) store(v, load(v));
         i0 = nv * 8;
     }
     for (int i = i0 + threadIdx.x; i < p.n; i += THR) {
@@ -155,10 +188,13 @@ __device__ __forceinline__ void scale_piece(const Piece& p, float c) {
     }
 }
 
-// The pieces in reverse: what the norm read last is still in the last-level cache.  The factor is worked out in fp64 and rounded once;
-// a NaN in it stays one.  A gradient that is its own result and needs no scaling is left alone.
-__global__ __launch_bounds__(THR) void k_grad_clip(const Piece* pieces, int64_t count, const double* sum_sq, float max_norm, float* norm) {
-    const double n = sqrt(*sum_sq), by = (double)max_norm / (n + 1e-6);
+// The pieces in reverse: what the norm read last is still in the last-level cache.  The sum of squares is *sum_sq, or (null) that of the
+// parts.  The factor is worked out in fp64 and rounded once; a NaN in it stays one.  A gradient that is its own result and needs no
+// scaling is left alone.
+__global__ __launch_bounds__(THR) void k_grad_clip(const Piece* __restrict__ pieces, int64_t count, const double* part, int parts, const double* sum_sq, float max_norm,
+                                                   float* norm) {
+    __shared__ double lds[4];
+    const double n = sqrt(sum_sq ? *sum_sq : sum_parts(part, parts, lds)), by = (double)max_norm / (n + 1e-6);
     const float c = by > 1.0 ? 1.f : (float)by;
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     for (int64_t k = count - 1 - blockIdx.x; k >= 0; k -= gridDim.x) {
@@ -175,7 +211,10 @@ __global__ __launch_bounds__(THR) void k_grad_clip(const Piece* pieces, int64_t 
 
 bool al(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 int64_t pieces_of(int64_t numel) { return (numel + PIECE - 1) / PIECE; }
-unsigned wgs_of(int64_t pieces) { return (unsigned)(pieces < 1 ? 1 : pieces < MAX_WGS ? pieces : MAX_WGS); }
+unsigned wgs_of(int64_t pieces, int most) { return (unsigned)(pieces < 1 ? 1 : pieces < most ? pieces : most); }
+void launch_squares(void* plan, int64_t pieces, hipStream_t st) {
+    hipLaunchKernelGGL(k_grad_squares, dim3(wgs_of(pieces, NORM_WGS)), dim3(THR), 0, st, (const Piece*)((Head*)plan + 1), pieces, ((Head*)plan)->part);
+}
 constexpr int64_t MAX_NUMEL = (int64_t)1 << 48;
 
 }  // namespace
@@ -230,7 +269,7 @@ extern "C" int ssd_grad_plan(int32_t ntensors, const ssd_grad_tensor_t* tensors,
             n += np;
         }
         const int64_t gx = (most + THR - 1) / THR;
-        hipLaunchKernelGGL(k_grad_pieces, dim3((unsigned)(gx < 1024 ? gx : 1024), t.count ? t.count : 1), dim3(THR), 0, st, t, list, head);
+        hipLaunchKernelGGL(k_grad_pieces, dim3((unsigned)(gx < 1024 ? gx : 1024), t.count ? t.count : 1), dim3(THR), 0, st, t, list);
     } while (i < ntensors);
     *pieces = n;
     return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
@@ -239,14 +278,18 @@ extern "C" int ssd_grad_plan(int32_t ntensors, const ssd_grad_tensor_t* tensors,
 extern "C" int ssd_grad_norm(void* plan, int64_t pieces, double* sum_sq, void* hip_stream) {
     if (!plan || !sum_sq) return SSD_ERR_NULL;
     if (pieces < 0 || !al(sum_sq, 8) || !al(plan, 256)) return SSD_ERR_ARG;
-    Head* head = (Head*)plan;
-    hipLaunchKernelGGL(k_grad_norm, dim3(wgs_of(pieces)), dim3(THR), 0, (hipStream_t)hip_stream, (const Piece*)(head + 1), pieces, head, sum_sq);
+    hipStream_t st = (hipStream_t)hip_stream;
+    launch_squares(plan, pieces, st);
+    hipLaunchKernelGGL(k_grad_sum, dim3(1), dim3(THR), 0, st, (const double*)plan, (int)wgs_of(pieces, NORM_WGS), sum_sq);
     return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
 }
 
 extern "C" int ssd_grad_clip(void* plan, int64_t pieces, const double* sum_sq, float max_norm, float* norm, void* hip_stream) {
-    if (!plan || !sum_sq) return SSD_ERR_NULL;
+    if (!plan) return SSD_ERR_NULL;
     if (pieces < 0 || !al(sum_sq, 8) || !al(norm, 4) || !al(plan, 256) || !(max_norm >= 0.f)) return SSD_ERR_ARG;
-    hipLaunchKernelGGL(k_grad_clip, dim3(wgs_of(pieces)), dim3(THR), 0, (hipStream_t)hip_stream, (const Piece*)((Head*)plan + 1), pieces, sum_sq, max_norm, norm);
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (!sum_sq) launch_squares(plan, pieces, st);
+    hipLaunchKernelGGL(k_grad_clip, dim3(wgs_of(pieces, CLIP_WGS)), dim3(THR), 0, st, (const Piece*)((Head*)plan + 1), pieces, (const double*)plan,
+                       (int)wgs_of(pieces, NORM_WGS), sum_sq, max_norm, norm);
     return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
 }
