@@ -334,7 +334,7 @@ __device__ __forceinline__ void turn_piece(const TurnJob& tj, const Plan& p, con
 }
 
 template <int RT, bool KROW>
-__global__ __launch_bounds__(64 * LWAVES) void k_low(LowParams lp, Plan p, const int* plan, TurnJob tj) {
+__global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, const int* plan, TurnJob tj) {
     extern __shared__ __attribute__((aligned(16))) char low_lds_mem[];
     if (KROW && (int)blockIdx.x < tj.blocks) {
         if (blockIdx.y == 0) turn_piece(tj, p, plan, blockIdx.x);

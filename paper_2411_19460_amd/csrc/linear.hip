@@ -726,25 +726,28 @@ GemmParams low_params(const LowProduct& j) {
 }
 
 // How a product with a low-rank term runs: few rows as products that stream w (few_rows.hip), some tens to hundreds in small tiles whose
-// waves share out K (split_rows.hip, 32 rows x 16 `width` columns), more in the tiles above, 64 `width` columns, K cut into `slices`
+// waves share out K (split_rows.hip, 16 mt rows x 16 `width` columns), more in the tiles above, 64 `width` columns, K cut into `slices`
 // where the tiles alone would leave compute units idle.  By the estimated time, us: a tile's K step of 64 columns x 4, 3, 2 takes 1.06,
 // 0.88, 0.67 and what surrounds the steps 7; slices cost a launch more (4) and their sums' way out and back (6 TB/s); a round of small
-// tiles costs 1 to 2 and, for each k, 1.1, 1.8, 2.4 ns at 16, 32, 64 columns (w with k as the row index: 2.2, 2.6, 3.0).  Measured
+// tiles costs 1 to 3 and, for each k, 1.1, 1.8, 2.4 ns at 16, 32, 64 columns (w with k as the row index: 2.2, 2.6, 3.0) and 3.6 at 64 x 64.  Measured
 // over 17 ... 4096 rows of five pairs of widths from 768 to 10576, small tiles / slices / whole tiles, narrow products included: 64 rows
-// 5120 -> 2560 19 / 28 / 64 us, 100 rows 25 / 31 / 65, 256 rows 40 / 36 / 67, 1000 rows - / 51 / 68, 4096 rows - / 113 / 99; 64 rows
-// 2560 -> 10576 25 / 31 / 40, 256 rows 60 / 38 / 42; input gradient of 2560 -> 10576, 32 rows 38 / 34 / 116, 256 rows 84 / 52 / 141,
+// 5120 -> 2560 20 / 28 / 64 us, 100 rows 25 / 31 / 65, 256 rows 31 / 36 / 67, 1000 rows - / 51 / 68, 4096 rows - / 113 / 99; 64 rows
+// 2560 -> 10576 21 / 31 / 40, 256 rows 46 / 38 / 42; input gradient of 2560 -> 10576, 32 rows 39 / 34 / 116, 256 rows 61 / 52 / 141,
 // 1000 rows - / 85 / 145.
 struct LowRun {
     enum { FEW, SMALL, TILES } kind;
-    int width, slices;
+    int mt, width, slices;
 };
 LowRun low_run(const GemmParams& gp, bool input_grad) {
-    if (!input_grad && gp.M <= FEW_ROWS && few_rows_supported(few_rows_job(gp))) return {LowRun::FEW, 0, 1};
-    constexpr double STEP[5] = {0, 0, 0.67, 0.88, 1.06}, ROUND[5] = {0, 1.2, 1.5, 0, 2.0};
-    constexpr double PER_K[2][5] = {{0, 0.0011, 0.0018, 0, 0.0024}, {0, 0.0022, 0.0026, 0, 0.0030}};
+    if (!input_grad && gp.M <= FEW_ROWS && few_rows_supported(few_rows_job(gp))) return {LowRun::FEW, 0, 0, 1};
+    constexpr double STEP[5] = {0, 0, 0.67, 0.88, 1.06};
+    static constexpr struct {
+        int mt, nt;
+        double round, per_k[2];
+    } SMALL[] = {{2, 1, 1.2, {0.0011, 0.0022}}, {2, 2, 1.5, {0.0018, 0.0026}}, {2, 4, 2.0, {0.0024, 0.0030}}, {4, 4, 3.0, {0.0036, 0.0036}}};
     const int steps = (gp.K + BKK - 1) / BKK;
     auto rounds = [](int64_t wgs) { return (double)((wgs + UNITS - 1) / UNITS); };
-    LowRun best = {LowRun::TILES, 0, 1};  // width 0: the rules of the plain products
+    LowRun best = {LowRun::TILES, 0, 0, 1};  // width 0: the rules of the plain products
     double t = 1e30;
     const int dw = input_grad ? 2 : 1;
     for (int w = 4; w >= 2; w -= dw) {
@@ -756,14 +759,15 @@ LowRun low_run(const GemmParams& gp, bool input_grad) {
         const int64_t tiles = tile_count(gp, w);
         for (int s = 2; s <= 16 && steps / s >= 4 && tiles * s <= 2 * UNITS; ++s) {
             const double c = rounds(tiles * s) * ((steps + s - 1) / s * STEP[w] + 7) + 4 + (double)s * gp.M * gp.N * 8 / 6e6;
-            if (c < t) t = c, best = {LowRun::TILES, w, s};
+            if (c < t) t = c, best = {LowRun::TILES, 0, w, s};
         }
     }
     if (best.slices == 1) t /= 0.9;
-    for (int w = 1; w <= 4; w *= 2) {
-        const int64_t wgs = (int64_t)((gp.M + 31) / 32) * ((gp.N + 16 * w - 1) / (16 * w));
-        const double c = 2 + rounds(wgs) * (ROUND[w] + PER_K[input_grad][w] * gp.K);
-        if (c < t) t = c, best = {LowRun::SMALL, w, 1};
+    for (const auto& sm : SMALL) {
+        if (gp.lda > MAX_LD || gp.ldb > MAX_LD) break;  // offsets of 32 bits
+        const int64_t wgs = (int64_t)((gp.M + 16 * sm.mt - 1) / (16 * sm.mt)) * ((gp.N + 16 * sm.nt - 1) / (16 * sm.nt));
+        const double c = 2 + rounds(wgs) * (sm.round + sm.per_k[input_grad] * gp.K);
+        if (c < t) t = c, best = {LowRun::SMALL, sm.mt, sm.nt, 1};
     }
     return best;
 }
@@ -803,7 +807,7 @@ hipError_t launch_linear_low(const LowProduct& j, const LowRankTerm& lr, void* p
         f.low = &lr;
         return launch_linear_few_rows(f, st);
     }
-    if (r.kind == LowRun::SMALL) return launch_split_rows(j.input_grad, gp.M, gp.K, gp.N, j.x, gp.lda, j.w, gp.ldb, j.out, gp.ldc, r.width, lr, st);
+    if (r.kind == LowRun::SMALL) return launch_split_rows(j.input_grad, gp.M, gp.K, gp.N, j.x, gp.lda, j.w, gp.ldb, j.out, gp.ldc, r.mt, r.width, lr, st);
     return j.input_grad ? launch_low_tiles<false>(gp, lr, r, part, st) : launch_low_tiles<true>(gp, lr, r, part, st);
 }
 }  // namespace ssdk

@@ -1,12 +1,10 @@
 // Products of some tens to hundreds of rows with a low-rank term (adapters): out = x w^T + low up^T, forward (w [N, K]) or the input's
 // gradient (w [K, N]).  The tiles of linear.hip, 256 rows high and one to a compute unit, leave most of the chip idle here and walk the
-// whole of K one step after another.  These are 32 rows high and 16 NT columns wide (16 MT rows; 64 were slower wherever the launch rule takes this kernel), and the eight waves of a workgroup share out K in steps
-// of 64: a wave fetches a step's rows as 128 contiguous bytes each, several steps at a time, turns them into operands through LDS of its
+// whole of K one step after another.  These are 32 x 16, 32, 64 or 64 x 64 (16 MT rows, 16 NT columns), and the eight waves of a workgroup share out K in steps
+// of 64: a wave fetches a step's rows as 128 contiguous bytes each, U steps at a time, turns them into operands through LDS of its
 // own without a barrier, and the waves' sums meet in LDS once, at the end, where they are rounded and leave.  The rows' adapters are
 // shared out as well: wave w adds numbers w, w + 8, ... of the tile's.
 // What bounds it: the operands' way from the L2 (each element of x is fetched N / (16 NT) times, each of w rows / (16 MT) times).
-#include <type_traits>
-
 #include "low_rank.h"
 #include "mfma_common.h"
 
@@ -37,71 +35,59 @@ constexpr int split_lds() {
 }
 
 template <int MT, int NT, bool KROW, int U>
-__global__ __launch_bounds__(64 * WAVES) void k_split(SplitParams sp, LowRankTerm lr) {
+__global__ __launch_bounds__(64 * WAVES, 2) void k_split(SplitParams sp, LowRankTerm lr) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
     const int r8 = lane >> 3, c8 = (lane & 7) * 8;  // fetching lanes: eight rows of 64 elements
     // the row tiles of the same columns one after another on one XCD
     const int n = gridDim.x, per = n >> 3, b = blockIdx.x, id = b < 8 * per ? (b & 7) * per + (b >> 3) : b;
     const int m0 = id % sp.tiles_m * 16 * MT, n0 = id / sp.tiles_m * 16 * NT;
-    const __bf16* xr[2 * MT];
-#pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
-        const int m = m0 + 8 * i + r8;
-        xr[i] = sp.x + (int64_t)(m < sp.M ? m : sp.M - 1) * sp.ldx + c8;
-    }
-    // w: rows of columns (2 NT accesses of eight), or 64 rows of k of 16 NT columns (2 NT accesses of 32 / NT rows)
+    // Rows and columns that do not exist, and k beyond K, are fetched from beyond a descriptor's end: zeros.
+    constexpr uint32_t OUT = 0x80000000u;
+    const uint32_t ldx = (uint32_t)sp.ldx * 2, ldw = (uint32_t)sp.ldw * 2;
+    const rsrc_t rx = make_rows(sp.x + m0 * sp.ldx, sp.M - m0 < 16 * MT ? sp.M - m0 : 16 * MT, ldx);
+    const uint32_t x0 = r8 * ldx + c8 * 2;
+    // w: 16 NT rows of 64 k, or 64 rows of k of 16 NT columns
     constexpr int CP = 2 * NT, KR = 64 / CP;  // KROW: pieces of a row, rows an access
-    const __bf16* wr[2 * NT];
-#pragma unroll
-    for (int i = 0; i < 2 * NT; ++i) {
-        if (KROW) {
-            const int c = n0 + 8 * (lane % CP);
-            wr[i] = sp.w + (int64_t)(i * KR + lane / CP) * sp.ldw + (c < sp.N ? c : 0);  // (columns beyond the end are not stored)
-        } else {
-            const int c = n0 + 8 * i + r8;
-            wr[i] = sp.w + (int64_t)(c < sp.N ? c : sp.N - 1) * sp.ldw + c8;
-        }
-    }
+    const rsrc_t rw = make_rows(sp.w + n0 * sp.ldw, sp.N - n0 < 16 * NT ? sp.N - n0 : 16 * NT, ldw);  // (KROW: not used)
+    const uint32_t w0 = !KROW ? r8 * ldw + c8 * 2 : n0 + 8 * (lane % CP) < sp.N ? (lane / CP) * ldw + (n0 + 8 * (lane % CP)) * 2 : OUT;
     char *mx = lds + wv * wave_lds<MT, NT, KROW>(), *mw = mx + 16 * MT * PITCH;
     f32x4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = (f32x4)(0.f);
-    const bf16x8 zero = (bf16x8)((__bf16)0.f);
-    bf16x8 xv[U][2 * MT], wf[U][2 * NT];
-    // The U steps from k0 on.  WHOLE: all of their k exist; else what lies beyond K comes from k = 0 and is put to zero (in both
-    // operands: an infinity there would be a NaN).
-    auto load = [&](int k0, auto whole) {
-        constexpr bool WHOLE = decltype(whole)::value;
+    struct Steps {
+        bf16x8 x[U][2 * MT], w[U][2 * NT];
+    };
+    auto load = [&](Steps& b, int k0) {
 #pragma unroll
         for (int s = 0; s < U; ++s) {
-            const int ks = k0 + 64 * WAVES * s, kc = WHOLE || ks + c8 < sp.K ? ks : -c8;
+            const int ks = k0 + 64 * WAVES * s;
+            const uint32_t off = ks + c8 < sp.K ? (uint32_t)ks * 2 : OUT;
 #pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) xv[s][i] = *(const bf16x8*)(xr[i] + kc);
+            for (int i = 0; i < 2 * MT; ++i) b.x[s][i] = rows_load(rx, x0 + off + i * 8 * ldx);
+            if (KROW) {
+                const int left = sp.K - ks;
+                const rsrc_t rk = make_rows(sp.w + (int64_t)(left > 0 ? ks : 0) * sp.ldw, left < 0 ? 0 : left < 64 ? left : 64, ldw);
 #pragma unroll
-            for (int i = 0; i < 2 * NT; ++i) {
-                if (KROW) wf[s][i] = *(const bf16x8*)(wr[i] + (WHOLE || ks + i * KR + lane / CP < sp.K ? (int64_t)ks : -(int64_t)(i * KR + lane / CP)) * sp.ldw);
-                else wf[s][i] = *(const bf16x8*)(wr[i] + kc);
+                for (int i = 0; i < 2 * NT; ++i) b.w[s][i] = rows_load(rk, w0 + i * KR * ldw);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2 * NT; ++i) b.w[s][i] = rows_load(rw, w0 + off + i * 8 * ldw);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto use = [&](int k0, auto whole) {
-        constexpr bool WHOLE = decltype(whole)::value;
+    auto use = [&](const Steps& b, int k0) {
 #pragma unroll
         for (int s = 0; s < U; ++s) {
-            const int ks = k0 + 64 * WAVES * s;
-            if (!WHOLE && ks >= sp.K) break;
-            const bool in = WHOLE || ks + c8 < sp.K;
+            if (k0 + 64 * WAVES * s >= sp.K) break;
 #pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) *(bf16x8*)(mx + (8 * i + r8) * PITCH + 2 * c8) = in ? xv[s][i] : zero;
+            for (int i = 0; i < 2 * MT; ++i) *(bf16x8*)(mx + (8 * i + r8) * PITCH + 2 * c8) = b.x[s][i];
 #pragma unroll
-            for (int i = 0; i < 2 * NT; ++i) {
-                if (KROW) *(bf16x8*)(mw + (i * KR + lane / CP) * krow_pitch<NT>() + 16 * (lane % CP)) = WHOLE || ks + i * KR + lane / CP < sp.K ? wf[s][i] : zero;
-                else *(bf16x8*)(mw + (8 * i + r8) * PITCH + 2 * c8) = in ? wf[s][i] : zero;
-            }
+            for (int i = 0; i < 2 * NT; ++i)
+                *(bf16x8*)(KROW ? mw + (i * KR + lane / CP) * krow_pitch<NT>() + 16 * (lane % CP) : mw + (8 * i + r8) * PITCH + 2 * c8) = b.w[s][i];
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own rows: its LDS operations are done in order
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -127,22 +113,16 @@ __global__ __launch_bounds__(64 * WAVES) void k_split(SplitParams sp, LowRankTer
             asm volatile("" ::: "memory");  // the next step's rows come in behind these reads
         }
     };
-    constexpr int REACH = 64 * (WAVES * (U - 1) + 1), NEXT = 64 * WAVES * U;
+    constexpr int NEXT = 64 * WAVES * U;
+    Steps a, c;
     int k0 = 64 * wv;
-    const bool any = k0 + REACH <= sp.K;
-    if (any) load(k0, std::true_type{});
+    load(a, k0);
     add_low_rank<MT, NT>(acc, lr, m0, sp.M, n0, sp.N, lane, wv, WAVES);
-    if (any) {
-        for (;;) {
-            use(k0, std::true_type{});
-            k0 += NEXT;
-            if (k0 + REACH > sp.K) break;
-            load(k0, std::true_type{});
-        }
-    }
-    if (k0 < sp.K) {
-        load(k0, std::false_type{});
-        use(k0, std::false_type{});
+    for (; k0 < sp.K; k0 += 2 * NEXT) {  // one group of steps is multiplied while the next is under way
+        load(c, k0 + NEXT);
+        use(a, k0);
+        load(a, k0 + 2 * NEXT);
+        use(c, k0 + NEXT);
     }
     __syncthreads();
     float* sums = (float*)lds;  // lane -> row l16 of tile i, four consecutive columns
@@ -186,16 +166,17 @@ hipError_t launch(SplitParams sp, const LowRankTerm& lr, hipStream_t st) {
 }
 
 template <bool KROW>
-hipError_t launch_width(const SplitParams& sp, int nt, const LowRankTerm& lr, hipStream_t st) {
-    return nt == 1 ? launch<2, 1, KROW, 4>(sp, lr, st) : nt == 2 ? launch<2, 2, KROW, 4>(sp, lr, st) : launch<2, 4, KROW, 2>(sp, lr, st);
+hipError_t launch_shape(const SplitParams& sp, int mt, int nt, const LowRankTerm& lr, hipStream_t st) {
+    if (mt == 4) return launch<4, 4, KROW, 1>(sp, lr, st);
+    return nt == 1 ? launch<2, 1, KROW, 2>(sp, lr, st) : nt == 2 ? launch<2, 2, KROW, 2>(sp, lr, st) : launch<2, 4, KROW, 1>(sp, lr, st);
 }
 
 }  // namespace
 
-hipError_t launch_split_rows(bool input_grad, int rows, int K, int N, const void* x, int64_t ldx, const void* w, int64_t ldw, void* out, int64_t ldo, int nt,
+hipError_t launch_split_rows(bool input_grad, int rows, int K, int N, const void* x, int64_t ldx, const void* w, int64_t ldw, void* out, int64_t ldo, int mt, int nt,
                              const LowRankTerm& lr, hipStream_t st) {
     const SplitParams sp = {(const __bf16*)x, (const __bf16*)w, (__bf16*)out, ldx, ldw, ldo, rows, N, K, 0};
-    return input_grad ? launch_width<true>(sp, nt, lr, st) : launch_width<false>(sp, nt, lr, st);
+    return input_grad ? launch_shape<true>(sp, mt, nt, lr, st) : launch_shape<false>(sp, mt, nt, lr, st);
 }
 
 }  // namespace ssdk

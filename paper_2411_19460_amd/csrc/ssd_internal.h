@@ -371,8 +371,8 @@ struct LowProduct {
 };
 size_t linear_low_bytes(const LowProduct& j);  // of `part` (x, w and out are not looked at but for whether they are null)
 hipError_t launch_linear_low(const LowProduct& j, const LowRankTerm& lr, void* part, hipStream_t st);
-// The same in tiles of 32 rows and 16 nt columns (nt 1, 2, 4; split_rows.hip), K and N of the product
-hipError_t launch_split_rows(bool input_grad, int rows, int K, int N, const void* x, int64_t ldx, const void* w, int64_t ldw, void* out, int64_t ldo, int nt,
+// The same in tiles of 16 mt rows and 16 nt columns (2 x 1, 2, 4 and 4 x 4; split_rows.hip), K and N of the product
+hipError_t launch_split_rows(bool input_grad, int rows, int K, int N, const void* x, int64_t ldx, const void* w, int64_t ldw, void* out, int64_t ldo, int mt, int nt,
                              const LowRankTerm& lr, hipStream_t st);
 
 // Generation (few_rows.hip): products and the block's middle steps for at most FEW_ROWS tokens, bf16 storage.
