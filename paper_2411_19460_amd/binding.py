@@ -568,26 +568,37 @@ def ssd_adapter_plan(row_adapter, nadapters: int) -> AdapterPlan:
     return AdapterPlan(buf, rows, nadapters)
 
 
-def _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, strides, *same_device) -> ssd_adapter_shape_t:
+# Shape descriptors of adapters' calls with the by-reference argument and the workspace's size (see _shapes).
+_adapter_shapes: dict = {}
+
+
+def _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, strides, is_backward, *same_device):
+    """(by-reference shape, bytes of workspace, rank) of a call whose operands fit together."""
     import torch
     if not isinstance(plan, AdapterPlan):
         raise ValueError("plan must be ssd_adapter_plan's")
-    rows = plan.rows
-    if a.dim() != 3 or b.dim() != 3 or a.dtype != torch.bfloat16 or b.dtype != torch.bfloat16 or not a.is_contiguous() or not b.is_contiguous():
+    bf16, n = torch.bfloat16, plan.nadapters
+    if a.dim() != 3 or b.dim() != 3 or a.dtype != bf16 or b.dtype != bf16 or not a.is_contiguous() or not b.is_contiguous():
         raise ValueError("a and b must be dense bf16 [nadapters, rank, in_dim] and [nadapters, out_dim, rank]")
-    n, rank, _ = a.shape
+    rank = a.shape[1]
     if a.shape != (n, rank, in_dim) or b.shape != (n, out_dim, rank):
-        raise ValueError(f"a must be [nadapters, rank, {in_dim}] and b [nadapters, {out_dim}, rank], got {tuple(a.shape)} and {tuple(b.shape)}")
+        raise ValueError(f"a must be [{n}, rank, {in_dim}] and b [{n}, {out_dim}, rank] (the plan's adapters), got {tuple(a.shape)} and {tuple(b.shape)}")
     if scale.dtype != torch.float32 or scale.shape != (n,) or not scale.is_contiguous():
         raise ValueError("scale must be a dense fp32 [nadapters] device tensor")
-    if plan.nadapters != n:
-        raise ValueError(f"the plan is of {plan.nadapters} adapters, a and b have {n}")
-    if w is not None and (w.dtype != torch.bfloat16 or w.shape != (out_dim, in_dim) or not w.is_contiguous()):
+    if w is not None and (w.dtype != bf16 or w.shape != (out_dim, in_dim) or not w.is_contiguous()):
         raise ValueError("w must be a dense [out_dim, in_dim] bf16 device tensor")
+    dev = x.get_device()
     for t in (a, b, scale, plan.buffer, w, *same_device):
-        if t is not None and t.device != x.device:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"all tensors must be on {x.device}, got {t.device}")
-    return ssd_adapter_shape_t(rows, in_dim, out_dim, rank, n, *strides)
+    key = (plan.rows, in_dim, out_dim, rank, n, strides, is_backward)
+    hit = _adapter_shapes.get(key)
+    if hit is None:
+        if len(_adapter_shapes) > 1024:
+            _adapter_shapes.clear()
+        ref = ctypes.byref(ssd_adapter_shape_t(plan.rows, in_dim, out_dim, rank, n, *strides))
+        hit = _adapter_shapes[key] = (ref, int(lib().ssd_adapter_workspace_bytes(ref, is_backward)), rank)
+    return hit
 
 
 def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False, hidden=None, workspace=None):
@@ -601,16 +612,16 @@ def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False,
     if out is None:
         out = torch.empty((rows, out_dim), dtype=torch.bfloat16, device=x.device)
     ldo = _rows_view(out, "out")
-    shape = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldo, 0), out, hidden)
+    shape, nbytes, rank = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldo, 0), 0, out, hidden)
     if rows != plan.rows or out.shape != (rows, out_dim):
         raise ValueError(f"x and out must have the plan's {plan.rows} rows and w's {out_dim} columns")
     if hidden is None and want_hidden:
-        hidden = torch.empty((rows, shape.rank), dtype=torch.float32, device=x.device)
+        hidden = torch.empty((rows, rank), dtype=torch.float32, device=x.device)
     if hidden is not None:
-        _check_hidden(hidden, rows, shape.rank)
+        _check_hidden(hidden, rows, rank)
     if workspace is None:
-        workspace = _workspace(int(lib().ssd_adapter_workspace_bytes(ctypes.byref(shape), 0)), x.device)
-    rc = lib().ssd_adapter_linear_fwd(ctypes.byref(shape), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(out),
+        workspace = _workspace(nbytes, x.device)
+    rc = lib().ssd_adapter_linear_fwd(shape, _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(out),
                                       _ptr(hidden), _ptr(workspace), workspace.numel(), _stream(x))
     if rc != 0:
         raise SSDError(rc, "ssd_adapter_linear_fwd")
@@ -634,7 +645,7 @@ def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=T
     if dx is None and want_dx:
         dx = torch.empty((rows, in_dim), dtype=torch.bfloat16, device=x.device)
     lddx = _rows_view(dx, "dx") if dx is not None else 0
-    shape = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldd, lddx), dout, dx, da, db, hidden)
+    shape, nbytes, rank = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldd, lddx), 1, dout, dx, da, db, hidden)
     if rows != plan.rows or dout.shape[0] != rows or (dx is not None and dx.shape != x.shape):
         raise ValueError(f"x, dout and dx must have the plan's {plan.rows} rows, dx as many columns as x")
     if (da is None) != (db is None):
@@ -645,10 +656,10 @@ def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=T
         if t is not None and (t.dtype != torch.float32 or t.shape != like.shape or not t.is_contiguous()):
             raise ValueError(f"{name} must be a dense fp32 {tuple(like.shape)} device tensor")
     if hidden is not None:
-        _check_hidden(hidden, rows, shape.rank)
+        _check_hidden(hidden, rows, rank)
     if workspace is None:
-        workspace = _workspace(int(lib().ssd_adapter_workspace_bytes(ctypes.byref(shape), 1)), x.device)
-    rc = lib().ssd_adapter_linear_bwd(ctypes.byref(shape), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(dout),
+        workspace = _workspace(nbytes, x.device)
+    rc = lib().ssd_adapter_linear_bwd(shape, _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(dout),
                                       _ptr(hidden), _ptr(dx), _ptr(da), _ptr(db), _ptr(workspace), workspace.numel(), flags, _stream(x))
     if rc != 0:
         raise SSDError(rc, "ssd_adapter_linear_bwd")

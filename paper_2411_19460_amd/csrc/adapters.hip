@@ -32,9 +32,9 @@ struct Plan {
     int64_t ids, perm, start, first_long, first_slot, short_u, long_u, tile_n, tile_a, counts, words;
 };
 
-int long_unit_of(int64_t rows) {  // about sixteen units where all rows share an adapter
+int long_unit_of(int64_t rows) {  // about sixteen units where all rows share an adapter, one where rows are few
     const int64_t u = (rows / 16 + 63) / 64 * 64;
-    return (int)(u < 512 ? 512 : u);
+    return (int)(rows <= 1024 ? 1024 : u < 512 ? 512 : u);
 }
 
 Plan plan_of(int64_t rows, int32_t n) {
@@ -44,7 +44,7 @@ Plan plan_of(int64_t rows, int32_t n) {
     p.long_unit = long_unit_of(rows);
     auto least = [](int64_t a, int64_t b) { return (int)(a < b ? a : b); };
     p.max_short = least(rows, rows / SHORT_UNIT + n + 1);
-    p.max_long = least(rows, rows / p.long_unit + n);
+    p.max_long = (int)(rows / p.long_unit + n);
     p.tiles = (int)((rows + LOW_TILE - 1) / LOW_TILE);
     int64_t at = 0;
     auto take = [&](int64_t words) {
@@ -59,7 +59,7 @@ Plan plan_of(int64_t rows, int32_t n) {
     p.first_slot = take(n + 1);   // partial sums of the gradients: adapters of several long units
     p.short_u = take(4 * (int64_t)p.max_short);
     p.long_u = take(4 * (int64_t)p.max_long);
-    p.tile_n = take(p.tiles);
+    p.tile_n = take(2 * (int64_t)p.tiles);
     p.tile_a = take((int64_t)p.tiles * LOW_TILE);
     p.counts = take(n + 1);
     p.words = at;
@@ -67,8 +67,7 @@ Plan plan_of(int64_t rows, int32_t n) {
 }
 // Adapters of several long units have at most two units for each long_unit of their rows.
 int64_t most_slots(const Plan& p) {
-    const int64_t s = 2 * ((int64_t)p.rows / p.long_unit);
-    return s < p.max_long ? s : p.max_long;
+    return p.rows <= p.long_unit ? 0 : 2 * ((int64_t)p.rows / p.long_unit);
 }
 
 constexpr int PTHR = 256;
@@ -103,7 +102,8 @@ __global__ __launch_bounds__(PTHR) void k_plan_count(Plan p, const int* row_adap
         for (int j = 0; j < LOW_TILE; ++j) place += lds[j] < a;
         if (first) plan[p.tile_a + (int64_t)blockIdx.x * LOW_TILE + place] = a;
         const int listed = block_sum(first, lds);
-        if (tid == 0) plan[p.tile_n + blockIdx.x] = listed;
+        if (tid == 0) plan[p.tile_n + 2 * blockIdx.x] = listed;
+        if (first && place == 0) plan[p.tile_n + 2 * blockIdx.x + 1] = a;
         return;
     }
     const int mine = blockIdx.x - p.tiles;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
     __shared__ int lds[4];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, a = blockIdx.x;
     auto shorts = [](int c) { return (c + SHORT_UNIT - 1) / SHORT_UNIT; };
-    auto longs = [&](int c) { return (c + p.long_unit - 1) / p.long_unit; };
+    auto longs = [&](int c) { return c ? (c + p.long_unit - 1) / p.long_unit : 1; };  // (an adapter without rows has one unit without any: its gradients are zeros)
     int start = 0, fs = 0, fl = 0, fp = 0;
     for (int b = tid; b < a; b += PTHR) {
         const int c = plan[p.counts + b], l = longs(c);
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
     fs = block_sum(fs, lds);
     fl = block_sum(fl, lds);
     fp = block_sum(fp, lds);
-    const int mine = plan[p.counts + a], ns = shorts(mine), nl = longs(mine);
+    const int mine = plan[p.counts + a], ns = shorts(mine), nl = a < p.n ? longs(mine) : 0;
     if (tid == 0) {
         plan[p.start + a] = start;
         plan[p.first_long + a] = fl;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
     Unit *su = (Unit*)(plan + p.short_u), *lu = (Unit*)(plan + p.long_u);
     if (a == p.n) {
         for (int u = fs + ns + tid; u < p.max_short; u += PTHR) su[u] = Unit{0, 0, 0, 0};
-        for (int u = fl + tid; u < p.max_long; u += PTHR) lu[u] = Unit{0, 0, 0, 0};
+        for (int u = fl + tid; u < p.max_long; u += PTHR) lu[u] = Unit{-1, 0, 0, 0};
     }
     int at = start;
     const int wanted = a < p.n ? a : -1;
@@ -163,7 +163,9 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
     __syncthreads();  // the rows are in place (for this workgroup), the units can say whether theirs follow one another
     const int* rows = plan + p.perm + start;
     auto unit = [&](int u, int len) {
-        Unit t = {a, start + u * len, mine - u * len < len ? mine - u * len : len, rows[u * len]};
+        Unit t = {a, start + u * len, mine - u * len < len ? mine - u * len : len, 0};
+        if (t.count == 0) return t;
+        t.row0 = rows[u * len];
         if (rows[u * len + t.count - 1] != t.row0 + t.count - 1) t.row0 = -1;  // (they ascend)
         return t;
     };
@@ -235,7 +237,7 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
         for (int i = 0; i < MT; ++i) acc[t][i] = (f32x4)(0.f);
     // U steps at a time: all that they need is asked for before the first is used.  WHOLE: all of their k exist; else what lies beyond K
     // comes from k = 0 and is put to zero (in both operands: an infinity there would be a NaN).
-    constexpr int U = RT == 4 ? 2 : 4;
+    constexpr int U = RT == 4 ? 2 : MT == 1 ? 6 : 4;
     const bf16x8 zero = (bf16x8)((__bf16)0.f);
     auto steps = [&](int k0, auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
@@ -376,7 +378,8 @@ hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, co
 
 template <bool KROW>
 hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* plan, const TurnJob& tj, hipStream_t st) {
-    if (lp.rank <= 16) return launch_low_rt<1, KROW>(lp, p, plan, tj, st);
+    // few units: a workgroup for every sixteen ranks, x fetched again
+    if (lp.rank <= 16 || p.max_short * ((lp.rank + 15) / 16) <= 256) return launch_low_rt<1, KROW>(lp, p, plan, tj, st);
     if (lp.rank <= 32) return launch_low_rt<2, KROW>(lp, p, plan, tj, st);
     return launch_low_rt<4, KROW>(lp, p, plan, tj, st);
 }
@@ -399,76 +402,82 @@ struct GradParams {
     GradJob job[2];  // 0: dA, 1: dB (transposed)
     int rank, accumulate;
 };
-constexpr int GCOLS = 128, GRANKS = 64, GXP = GCOLS * 2 + 16, GSP = GRANKS * 2 + 16;
+// In LDS a row of X is 256 bytes, eight blocks of sixteen columns; a row of S holds its three parts in blocks of sixteen ranks, eight or
+// (RT 4) sixteen.  Half a wave's transposing read takes one block of each of the rows 0 .. 3 and 8 .. 11 of a step's sixteen: block b of
+// row k lies at place b ^ (k % 4 + 4 (k / 8 % 2)), which spreads them over all banks.
+constexpr int GCOLS = 128;
+constexpr int s_row(int rt) { return rt == 4 ? 512 : 256; }
+__device__ __forceinline__ int block_at(int k, int block) { return 32 * (block ^ ((k & 3) + ((k >> 1) & 4))); }
 
 template <int RT, bool TRANS>
 __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& gp, const Plan& p, const int* plan, const Unit un, int u, int cb, int r0, char* lds) {
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
     const int a = un.a, cnt = un.count, fl = plan[p.first_long + a], nl = plan[p.first_long + a + 1] - fl;
     const int* perm = plan + p.perm + un.first;
     auto row = [&](int t) -> int64_t { return un.row0 < 0 ? perm[t] : un.row0 + t; };
     const int c0 = cb * GCOLS;
-    char *lx = lds, *ls = lds + 64 * GXP;
+    char *lx = lds, *ls = lds + 64 * 256;
     f32x4 acc[RT][2];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[t][j] = (f32x4)(0.f);
-    bf16x8 xv[4];
-    f32x4 sv[RT];
-    auto load = [&](int t0) {
+    struct Rows {
+        bf16x8 x[4];
+        f32x4 s[RT];
+    };
+    auto load = [&](Rows& w, int t0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // 64 rows of 16 pieces
             const int v = i * 256 + tid, t = v >> 4, c = (v & 15) * 8;
-            xv[i] = (bf16x8)((__bf16)0.f);
-            if (t0 + t < cnt && c0 + c < jb.cols) xv[i] = *(const bf16x8*)(jb.x + row(t0 + t) * jb.ldx + c0 + c);
+            w.x[i] = (bf16x8)((__bf16)0.f);
+            if (t0 + t < cnt && c0 + c < jb.cols) w.x[i] = *(const bf16x8*)(jb.x + row(t0 + t) * jb.ldx + c0 + c);
         }
 #pragma unroll
         for (int i = 0; i < RT; ++i) {  // 64 rows of 4 RT pieces of four ranks
             const int v = i * 256 + tid, t = v / (4 * RT), r = 4 * (v % (4 * RT));
-            sv[i] = (f32x4)(0.f);
-            if (t0 + t < cnt && r0 + r < gp.rank) sv[i] = *(const f32x4*)(jb.s + row(t0 + t) * gp.rank + r0 + r);
+            w.s[i] = (f32x4)(0.f);
+            if (t0 + t < cnt && r0 + r < gp.rank) w.s[i] = *(const f32x4*)(jb.s + row(t0 + t) * gp.rank + r0 + r);
         }
     };
-    load(0);
-    for (int t0 = 0; t0 < cnt; t0 += 64) {
+    auto use = [&](Rows& w, int next) {
         __syncthreads();  // the operands before these have been read
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int v = i * 256 + tid;
-            *(bf16x8*)(lx + (v >> 4) * GXP + (v & 15) * 16) = xv[i];
+            *(bf16x8*)(lx + (v >> 4) * 256 + block_at(v >> 4, (v & 15) >> 1) + (v & 1) * 16) = w.x[i];
         }
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int v = i * 256 + tid, t = v / (4 * RT), r = 4 * (v % (4 * RT));
 #pragma unroll
             for (int part = 0; part < 3; ++part) {
-                const bf16x4 b = __builtin_convertvector(sv[i], bf16x4);
+                const bf16x4 b = __builtin_convertvector(w.s[i], bf16x4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sv[i][e] = __builtin_isinf((float)b[e]) ? 0.f : sv[i][e] - (float)b[e];  // (an infinity: the first part alone)
-                *(bf16x4*)(ls + (part * 64 + t) * GSP + 2 * r) = b;
+                for (int e = 0; e < 4; ++e) w.s[i][e] = __builtin_isinf((float)b[e]) ? 0.f : w.s[i][e] - (float)b[e];  // (an infinity: the first part alone)
+                *(bf16x4*)(ls + t * s_row(RT) + block_at(t, part * RT + (r >> 4)) + 2 * (r & 15)) = b;
             }
         }
         __syncthreads();
-        load(t0 + 64);  // the next rows come in while these are multiplied
+        load(w, next);  // two steps ahead
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int k = 32 * h + 8 * q + (l16 >> 2);
             bf16x8 xo[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const char* at = lx + k * GXP + (w * 32 + j * 16) * 2 + 8 * (l16 & 3);
+                const char* at = lx + k * 256 + block_at(k, 2 * wv + j) + 8 * (l16 & 3);
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * GXP));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * 256));  // (the same place: k + 4)
                 xo[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
 #pragma unroll
             for (int part = 0; part < 3; ++part)
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
-                    const char* at = ls + (part * 64 + k) * GSP + 32 * t + 8 * (l16 & 3);
+                    const char* at = ls + k * s_row(RT) + block_at(k, part * RT + t) + 8 * (l16 & 3);
                     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * GSP));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * s_row(RT)));
                     const bf16x8 so = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
@@ -476,6 +485,13 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
                                           : __builtin_amdgcn_mfma_f32_16x16x32_bf16(xo[j], so, acc[t][j], 0, 0, 0);
                 }
         }
+    };
+    Rows ra, rb;
+    load(ra, 0);
+    load(rb, 64);
+    for (int t0 = 0; t0 < cnt; t0 += 128) {
+        use(ra, t0 + 128);
+        if (t0 + 64 < cnt) use(rb, t0 + 192);
     }
     // TRANS: lane -> column l16, four consecutive ranks; else lane -> rank l16, four consecutive columns
     const bool direct = nl == 1;
@@ -485,7 +501,7 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int r = r0 + 16 * t + (TRANS ? 4 * q : l16), c = c0 + w * 32 + j * 16 + (TRANS ? l16 : 4 * q);
+            const int r = r0 + 16 * t + (TRANS ? 4 * q : l16), c = c0 + wv * 32 + j * 16 + (TRANS ? l16 : 4 * q);
             if (r >= gp.rank || c >= jb.cols) continue;
             f32x4* at = (f32x4*)(org + (TRANS ? (int64_t)c * gp.rank + r : (int64_t)r * jb.cols + c));
             *at = direct && gp.accumulate ? *at + acc[t][j] : acc[t][j];
@@ -494,20 +510,20 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
 
 template <int RT>
 __global__ __launch_bounds__(256) void k_adapter_grads(GradParams gp, Plan p, const int* plan) {
-    __shared__ __attribute__((aligned(16))) char lds[64 * GXP + 3 * 64 * GSP];
+    __shared__ __attribute__((aligned(16))) char lds[64 * (256 + s_row(RT))];
     const int u = blockIdx.y;
     const Unit un = ((const Unit*)(plan + p.long_u))[u];
-    if (un.count == 0) return;
+    if (un.a < 0) return;
     const int b = blockIdx.x, r0 = blockIdx.z * 16 * RT;
     if (b < gp.job[0].blocks) grad_unit<RT, false>(gp.job[0], gp, p, plan, un, u, b, r0, lds);
     else grad_unit<RT, true>(gp.job[1], gp, p, plan, un, u, b - gp.job[0].blocks, r0, lds);
 }
 
-// Adapters of several units: their sums in order; adapters without a row: zeros.
+// Adapters of several units: their sums in order.
 __global__ __launch_bounds__(256) void k_adapter_grads_sum(GradParams gp, Plan p, const int* plan, int blocks0) {
     const int a = blockIdx.y;
     const int nl = plan[p.first_long + a + 1] - plan[p.first_long + a];
-    if (nl == 1 || (nl == 0 && gp.accumulate)) return;
+    if (nl == 1) return;
     const GradJob& jb = gp.job[(int)blockIdx.x < blocks0 ? 0 : 1];
     const int64_t size = (int64_t)gp.rank * jb.cols;
     const int64_t i = ((int64_t)(blockIdx.x - ((int)blockIdx.x < blocks0 ? 0 : blocks0)) * 256 + threadIdx.x) * 4;
@@ -653,6 +669,7 @@ extern "C" int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const vo
     gp.accumulate = accumulate;
     const hipError_t e = gp.rank <= 16 ? launch_grads_rt<1>(gp, p, pl, st) : gp.rank <= 32 ? launch_grads_rt<2>(gp, p, pl, st) : launch_grads_rt<4>(gp, p, pl, st);
     if (e != hipSuccess) return SSD_ERR_LAUNCH;
+    if (!most_slots(p)) return SSD_OK;  // no adapter has several units
     const int64_t b0 = ((int64_t)gp.rank * shape->in_dim + 1023) / 1024, b1 = ((int64_t)gp.rank * shape->out_dim + 1023) / 1024;
     hipLaunchKernelGGL(k_adapter_grads_sum, dim3((unsigned)(b0 + b1), shape->nadapters), dim3(256), 0, st, gp, p, pl, (int)b0);
     return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;

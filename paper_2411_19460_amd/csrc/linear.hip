@@ -468,6 +468,99 @@ __global__ __launch_bounds__(GTHR, 1) void k_gemm_low_mixed(GemmParams p1, GemmP
     else gemm_tile<true, true, W2, true>(p2, blockIdx.x - first, &lr2);
 }
 
+// 128 x 128 tiles for products whose 256-row tiles are too few (600 rows 1024 -> 4384 25 -> 21 us, 1000 rows 768 -> 3352 22 -> 18, narrow
+// product included; in more than one round the 256-row tiles are faster): eight waves of 64 x 32, four buffers of a K step, loaded three steps
+// ahead, one barrier a step (the waves have left step t - 1: step t + 3 may come in where it was).
+template <bool BK>
+struct Half {
+    typedef Tile<128, true> TA;
+    typedef Tile<128, BK> TB;
+    static constexpr int STAGE = TA::BYTES + TB::BYTES, STAGES = 4, LOADS = TA::LOADS + TB::LOADS, LDS = STAGES * STAGE;
+    static __device__ __forceinline__ void multiply(const char* st, int wm, int wn, int lane, f32x4 (&acc)[4][2]) {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            bf16x8 a[4], b[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) b[j] = TB::operand(st + TA::BYTES, wn * 32 + j * 16, ks, lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = TA::operand(st, wm * 64 + i * 16, ks, lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+        }
+    }
+};
+
+template <bool BK>
+__device__ __forceinline__ void half_tile(const GemmParams& gp, int id, const LowRankTerm& lr) {
+    typedef Half<BK> H;
+    typedef typename H::TA TA;
+    typedef typename H::TB TB;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w >> 2, wn = w & 3;
+    int tm, tn;
+    tile_of(gp, id, tm, tn);
+    const int m0 = tm * 128, n0 = tn * 128, rows_a = gp.M - m0, rows_b = gp.N - n0;
+    const bf16_t *a_org = gp.A + (int64_t)m0 * gp.lda, *b_org = BK ? gp.B + (int64_t)n0 * gp.ldb : gp.B + n0;
+    const uint32_t va = TA::voff(gp.lda, rows_a, tid), vb = TB::voff(gp.ldb, rows_b, tid);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    f32x4 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = (f32x4)(0.f);
+    const int steps = gp.K / BKK;
+    auto issue = [&](int t) {
+        const uint32_t at = lds0 + (t % H::STAGES) * H::STAGE;
+        const u32x4 sa = TA::span(a_org + (int64_t)t * BKK, gp.lda, rows_a), sb = TB::span(b_org + (int64_t)t * BKK * (BK ? 1 : gp.ldb), gp.ldb, rows_b);
+        TA::template load<0>(sa, gp.lda, va, at, w);
+        TA::template load<1>(sa, gp.lda, va, at, w);
+        TB::template load<0>(sb, gp.ldb, vb, at + TA::BYTES, w);
+        TB::template load<1>(sb, gp.ldb, vb, at + TA::BYTES, w);
+    };
+    static_assert(TA::LOADS == 2 && TB::LOADS == 2, "");
+    for (int t = 0; t < 3 && t < steps; ++t) issue(t);
+    add_low_rank<4, 2>(acc, lr, m0 + wm * 64, gp.M, n0 + wn * 32, gp.N, lane, 0, 1);
+    wait_loads();  // see gemm_tile
+    int t = 0;
+    for (; t + 3 < steps; ++t) {
+        wait_and_meet<2 * H::LOADS>();
+        issue(t + 3);
+        H::multiply(lds + (t % H::STAGES) * H::STAGE, wm, wn, lane, acc);
+    }
+    for (; t < steps; ++t) {
+        wait_and_meet<0>();
+        H::multiply(lds + (t % H::STAGES) * H::STAGE, wm, wn, lane, acc);
+    }
+    const int left = gp.K - steps * BKK;
+    if (left) {  // through registers: k beyond the end has to read as zero
+        __syncthreads();
+        TA::load_part(a_org + (int64_t)steps * BKK, gp.lda, rows_a, left, lds, tid);
+        TB::load_part(b_org + (int64_t)steps * BKK * (BK ? 1 : gp.ldb), gp.ldb, rows_b, left, lds + TA::BYTES, tid);
+        __syncthreads();
+        H::multiply(lds, wm, wn, lane, acc);
+    }
+    const int row0 = m0 + wm * 64, col0 = n0 + wn * 32, l16 = lane & 15, q = lane >> 4;
+    __syncthreads();  // as in gemm_tile: each wave turns its own tile in a patch
+    constexpr int EPITCH = 64 + 16;
+    char* patch = lds + w * (64 * EPITCH);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *(bf16x4*)(patch + (i * 16 + l16) * EPITCH + (j * 16 + q * 4) * 2) = __builtin_convertvector(acc[i][j], bf16x4);
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int v = it * 64 + lane, r = v >> 2, c = v & 3, row = row0 + r, col = col0 + c * 8;
+        const bf16x8 o = *(const bf16x8*)(patch + r * EPITCH + c * 16);
+        if (row < gp.M && col < gp.N) *(bf16x8*)((__bf16*)gp.C + (int64_t)row * gp.ldc + col) = o;
+    }
+}
+
+template <bool BK>
+__global__ __launch_bounds__(GTHR, 1) void k_half_low(GemmParams gp, LowRankTerm lr) {
+    half_tile<BK>(gp, blockIdx.x, lr);
+}
+
 // K in `slices` pieces of k_slice: slice s of a tile leaves its sums in fp32 at part + s M N (the low-rank term with the first).
 template <bool BK, int WJ>
 __global__ __launch_bounds__(GTHR, 1) void k_gemm_low_slices(GemmParams gp, LowRankTerm lr, int k_slice) {
@@ -654,6 +747,18 @@ hipError_t launch_low(GemmParams gp, const LowRankTerm& lr, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <bool BK>
+hipError_t launch_half(GemmParams gp, const LowRankTerm& lr, hipStream_t st) {
+    constexpr int LDS = Half<BK>::LDS;
+    static bool raised[64];
+    const hipError_t e = allow_lds((const void*)k_half_low<BK>, LDS, raised);
+    if (e != hipSuccess) return e;
+    gp.tiles_m = (gp.M + 127) / 128;
+    gp.tiles_n = (gp.N + 127) / 128;
+    hipLaunchKernelGGL((k_half_low<BK>), dim3(gp.tiles_m * gp.tiles_n), dim3(GTHR), LDS, st, gp, lr);
+    return hipGetLastError();
+}
+
 template <int W1, int W2>
 hipError_t launch_low_mixed(GemmParams gp, int n1, const LowRankTerm& lr, hipStream_t st) {
     constexpr int L1 = big_lds<true, true, W1>(), L2 = big_lds<true, true, W2>(), LDS = L1 > L2 ? L1 : L2;
@@ -728,14 +833,14 @@ GemmParams low_params(const LowProduct& j) {
 // How a product with a low-rank term runs: few rows as products that stream w (few_rows.hip), some tens to hundreds in small tiles whose
 // waves share out K (split_rows.hip, 16 mt rows x 16 `width` columns), more in the tiles above, 64 `width` columns, K cut into `slices`
 // where the tiles alone would leave compute units idle.  By the estimated time, us: a tile's K step of 64 columns x 4, 3, 2 takes 1.06,
-// 0.88, 0.67 and what surrounds the steps 7; slices cost a launch more (4) and their sums' way out and back (6 TB/s); a round of small
+// 0.88, 0.67 (128 x 128: 0.52) and what surrounds the steps 7 (6); slices cost a launch more (4) and their sums' way out and back (6 TB/s); a round of small
 // tiles costs 1 to 3 and, for each k, 1.1, 1.8, 2.4 ns at 16, 32, 64 columns (w with k as the row index: 2.2, 2.6, 3.0) and 3.6 at 64 x 64.  Measured
 // over 17 ... 4096 rows of five pairs of widths from 768 to 10576, small tiles / slices / whole tiles, narrow products included: 64 rows
 // 5120 -> 2560 20 / 28 / 64 us, 100 rows 25 / 31 / 65, 256 rows 31 / 36 / 67, 1000 rows - / 51 / 68, 4096 rows - / 113 / 99; 64 rows
 // 2560 -> 10576 21 / 31 / 40, 256 rows 46 / 38 / 42; input gradient of 2560 -> 10576, 32 rows 39 / 34 / 116, 256 rows 61 / 52 / 141,
 // 1000 rows - / 85 / 145.
 struct LowRun {
-    enum { FEW, SMALL, TILES } kind;
+    enum { FEW, SMALL, HALF, TILES } kind;
     int mt, width, slices;
 };
 LowRun low_run(const GemmParams& gp, bool input_grad) {
@@ -754,6 +859,8 @@ LowRun low_run(const GemmParams& gp, bool input_grad) {
         const double one = rounds(tile_count(gp, w)) * (steps * STEP[w] + 7);
         if (one < t) t = one;
     }
+    const double half = rounds((int64_t)((gp.M + 127) / 128) * ((gp.N + 127) / 128)) * (steps * 0.52 + 6);
+    if (half < t && gp.lda <= MAX_LD && gp.ldb <= MAX_LD) t = half, best = {LowRun::HALF, 0, 0, 1};
     t *= 0.9;  // slices for a tenth at least
     for (int w = 4; w >= 2; w -= dw) {
         const int64_t tiles = tile_count(gp, w);
@@ -808,6 +915,7 @@ hipError_t launch_linear_low(const LowProduct& j, const LowRankTerm& lr, void* p
         return launch_linear_few_rows(f, st);
     }
     if (r.kind == LowRun::SMALL) return launch_split_rows(j.input_grad, gp.M, gp.K, gp.N, j.x, gp.lda, j.w, gp.ldb, j.out, gp.ldc, r.mt, r.width, lr, st);
+    if (r.kind == LowRun::HALF) return j.input_grad ? launch_half<false>(gp, lr, st) : launch_half<true>(gp, lr, st);
     return j.input_grad ? launch_low_tiles<false>(gp, lr, r, part, st) : launch_low_tiles<true>(gp, lr, r, part, st);
 }
 }  // namespace ssdk

@@ -14,7 +14,7 @@ namespace ssdk {
 template <int MT, int NT, int UB = 1>
 static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], const LowRankTerm& lr, int m0, int M, int n0, int N, int lane, int u0, int ustep) {
     using namespace mf;
-    const int tile = m0 / LOW_TILE, nu = lr.tile_n[tile], q = lane >> 4, l16 = lane & 15;
+    const int tile = m0 / LOW_TILE, nu = lr.tile_n[2 * tile], a0 = lr.tile_n[2 * tile + 1], q = lane >> 4, l16 = lane & 15;
     if (u0 >= nu) return;
     const int* list = lr.tile_a + (int64_t)tile * LOW_TILE;
     int of_row[MT];
@@ -40,7 +40,7 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
         for (int u = u0; u < nu; u += UB * ustep) {
             int ad[UB];
 #pragma unroll
-            for (int v = 0; v < UB; ++v) ad[v] = u + v * ustep < nu ? list[u + v * ustep] : -2;
+            for (int v = 0; v < UB; ++v) ad[v] = u + v * ustep < nu ? u + v * ustep ? list[u + v * ustep] : a0 : -2;
             if (UB == 1) {
                 bool any = false;
 #pragma unroll
