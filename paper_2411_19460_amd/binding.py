@@ -568,37 +568,56 @@ def ssd_adapter_plan(row_adapter, nadapters: int) -> AdapterPlan:
     return AdapterPlan(buf, rows, nadapters)
 
 
-# Shape descriptors of adapters' calls with the by-reference argument and the workspace's size (see _shapes).
-_adapter_shapes: dict = {}
+# Adapters' calls whose operands fit together, by what these are (sizes, strides, types, devices): the by-reference shape, the rank and
+# the workspace's size.  The checks cost as much as a launch; bounded, read only.
+_adapter_calls: dict = {}
 
 
-def _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, strides, is_backward, *same_device):
-    """(by-reference shape, bytes of workspace, rank) of a call whose operands fit together."""
-    import torch
+def _sig(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+def _adapter_call(plan, x, w, a, b, scale, rows_out, hidden, dx=None, da=None, db=None, is_backward=0):
+    """rows_out: out (None: dense) or dout."""
     if not isinstance(plan, AdapterPlan):
         raise ValueError("plan must be ssd_adapter_plan's")
-    bf16, n = torch.bfloat16, plan.nadapters
-    if a.dim() != 3 or b.dim() != 3 or a.dtype != bf16 or b.dtype != bf16 or not a.is_contiguous() or not b.is_contiguous():
-        raise ValueError("a and b must be dense bf16 [nadapters, rank, in_dim] and [nadapters, out_dim, rank]")
-    rank = a.shape[1]
-    if a.shape != (n, rank, in_dim) or b.shape != (n, out_dim, rank):
-        raise ValueError(f"a must be [{n}, rank, {in_dim}] and b [{n}, {out_dim}, rank] (the plan's adapters), got {tuple(a.shape)} and {tuple(b.shape)}")
-    if scale.dtype != torch.float32 or scale.shape != (n,) or not scale.is_contiguous():
-        raise ValueError("scale must be a dense fp32 [nadapters] device tensor")
-    if w is not None and (w.dtype != bf16 or w.shape != (out_dim, in_dim) or not w.is_contiguous()):
-        raise ValueError("w must be a dense [out_dim, in_dim] bf16 device tensor")
-    dev = x.get_device()
-    for t in (a, b, scale, plan.buffer, w, *same_device):
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"all tensors must be on {x.device}, got {t.device}")
-    key = (plan.rows, in_dim, out_dim, rank, n, strides, is_backward)
-    hit = _adapter_shapes.get(key)
+    key = (is_backward, plan.rows, plan.nadapters, plan.buffer.get_device(), _sig(x), _sig(w), _sig(a), _sig(b), _sig(scale), _sig(rows_out),
+           _sig(hidden), _sig(dx), _sig(da), _sig(db))
+    hit = _adapter_calls.get(key)
     if hit is None:
-        if len(_adapter_shapes) > 1024:
-            _adapter_shapes.clear()
-        ref = ctypes.byref(ssd_adapter_shape_t(plan.rows, in_dim, out_dim, rank, n, *strides))
-        hit = _adapter_shapes[key] = (ref, int(lib().ssd_adapter_workspace_bytes(ref, is_backward)), rank)
+        if len(_adapter_calls) > 1024:
+            _adapter_calls.clear()
+        hit = _adapter_calls[key] = _adapter_check(plan, x, w, a, b, scale, rows_out, hidden, dx, da, db, is_backward)
     return hit
+
+
+def _adapter_check(plan, x, w, a, b, scale, rows_out, hidden, dx, da, db, is_backward):
+    import torch
+    ldx = _rows_view(x, "x")
+    rows, in_dim = x.shape
+    out_dim = rows_out.shape[1] if is_backward and rows_out.dim() == 2 else w.shape[0] if w.dim() == 2 else -1
+    n, bf16 = plan.nadapters, torch.bfloat16
+    for name, t, shape, dtype in (("w", w, (out_dim, in_dim), bf16), ("a", a, (n, a.shape[1] if a.dim() == 3 else 0, in_dim), bf16),
+                                  ("b", b, (n, out_dim, a.shape[1] if a.dim() == 3 else 0), bf16), ("scale", scale, (n,), torch.float32),
+                                  ("hidden", hidden, (rows, a.shape[1] if a.dim() == 3 else 0), torch.float32),
+                                  ("da", da, a.shape, torch.float32), ("db", db, b.shape, torch.float32)):
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a dense {dtype} {tuple(shape)} device tensor (plan: {plan.rows} rows, {n} adapters), got {t.dtype} {tuple(t.shape)}")
+    if (da is None) != (db is None):
+        raise ValueError("da and db: both or neither")
+    strides = [ldx, 0, 0]
+    for i, (name, t, cols) in enumerate((("dout" if is_backward else "out", rows_out, out_dim), ("dx", dx, in_dim))):
+        if t is not None:
+            strides[1 + i] = _rows_view(t, name)
+            if t.shape != (rows, cols):
+                raise ValueError(f"{name} must be [{rows}, {cols}], got {tuple(t.shape)}")
+    if rows != plan.rows:
+        raise ValueError(f"the plan is of {plan.rows} rows, x has {rows}")
+    for t in (w, a, b, scale, plan.buffer, rows_out, hidden, dx, da, db):
+        if t is not None and t.device != x.device:
+            raise ValueError(f"all tensors must be on {x.device}, got {t.device}")
+    ref = ctypes.byref(ssd_adapter_shape_t(rows, in_dim, out_dim, a.shape[1], n, *strides))
+    return ref, a.shape[1], max(256, int(lib().ssd_adapter_workspace_bytes(ref, is_backward)))
 
 
 def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False, hidden=None, workspace=None):
@@ -606,32 +625,19 @@ def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False,
     ssd_adapter_plan's).  a [nadapters, rank, in_dim], b [nadapters, out_dim, rank], scale [nadapters] fp32.  `hidden` is h, fp32
     [rows, rank], kept for ssd_adapter_linear_bwd where want_hidden is set or the tensor given, else None."""
     import torch
-    ldx = _rows_view(x, "x")
-    rows, in_dim = x.shape
-    out_dim = w.shape[0]
+    shape, rank, nbytes = _adapter_call(plan, x, w, a, b, scale, out, hidden)
+    rows, dev = plan.rows, x.device
     if out is None:
-        out = torch.empty((rows, out_dim), dtype=torch.bfloat16, device=x.device)
-    ldo = _rows_view(out, "out")
-    shape, nbytes, rank = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldo, 0), 0, out, hidden)
-    if rows != plan.rows or out.shape != (rows, out_dim):
-        raise ValueError(f"x and out must have the plan's {plan.rows} rows and w's {out_dim} columns")
+        out = torch.empty((rows, w.shape[0]), dtype=torch.bfloat16, device=dev)
     if hidden is None and want_hidden:
-        hidden = torch.empty((rows, rank), dtype=torch.float32, device=x.device)
-    if hidden is not None:
-        _check_hidden(hidden, rows, rank)
+        hidden = torch.empty((rows, rank), dtype=torch.float32, device=dev)
     if workspace is None:
-        workspace = _workspace(nbytes, x.device)
-    rc = lib().ssd_adapter_linear_fwd(shape, _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(out),
-                                      _ptr(hidden), _ptr(workspace), workspace.numel(), _stream(x))
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    rc = lib().ssd_adapter_linear_fwd(shape, x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scale.data_ptr(), plan.buffer.data_ptr(),
+                                      out.data_ptr(), _ptr(hidden), workspace.data_ptr(), workspace.numel(), _stream(x))
     if rc != 0:
         raise SSDError(rc, "ssd_adapter_linear_fwd")
     return {"out": out, "hidden": hidden}
-
-
-def _check_hidden(hidden, rows, rank):
-    import torch
-    if hidden.dtype != torch.float32 or hidden.shape != (rows, rank) or not hidden.is_contiguous():
-        raise ValueError("hidden must be a dense fp32 [rows, rank] device tensor")
 
 
 def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=True, want_dab=True, flags=0, dx=None, da=None, db=None,
@@ -639,28 +645,17 @@ def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=T
     """dict(dx, da, db) for the loss <dout, out>; da and db are fp32, shaped as a and b; w is frozen (its gradient is ssd_linear_bwd's).
     `hidden`: the forward call's, worked out again if None."""
     import torch
-    ldx, ldd = _rows_view(x, "x"), _rows_view(dout, "dout")
-    rows, in_dim = x.shape
-    out_dim = dout.shape[1]
+    shape, _, nbytes = _adapter_call(plan, x, w, a, b, scale, dout, hidden, dx, da, db, 1)
+    dev = x.device
     if dx is None and want_dx:
-        dx = torch.empty((rows, in_dim), dtype=torch.bfloat16, device=x.device)
-    lddx = _rows_view(dx, "dx") if dx is not None else 0
-    shape, nbytes, rank = _adapter_shape(x, a, b, scale, plan, w, in_dim, out_dim, (ldx, ldd, lddx), 1, dout, dx, da, db, hidden)
-    if rows != plan.rows or dout.shape[0] != rows or (dx is not None and dx.shape != x.shape):
-        raise ValueError(f"x, dout and dx must have the plan's {plan.rows} rows, dx as many columns as x")
-    if (da is None) != (db is None):
-        raise ValueError("da and db: both or neither")
+        dx = torch.empty(x.shape, dtype=torch.bfloat16, device=dev)
     if da is None and want_dab:
-        da, db = (torch.empty(t.shape, dtype=torch.float32, device=x.device) for t in (a, b))
-    for name, t, like in (("da", da, a), ("db", db, b)):
-        if t is not None and (t.dtype != torch.float32 or t.shape != like.shape or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a dense fp32 {tuple(like.shape)} device tensor")
-    if hidden is not None:
-        _check_hidden(hidden, rows, rank)
+        da, db = torch.empty(a.shape, dtype=torch.float32, device=dev), torch.empty(b.shape, dtype=torch.float32, device=dev)
     if workspace is None:
-        workspace = _workspace(nbytes, x.device)
-    rc = lib().ssd_adapter_linear_bwd(shape, _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.buffer), _ptr(dout),
-                                      _ptr(hidden), _ptr(dx), _ptr(da), _ptr(db), _ptr(workspace), workspace.numel(), flags, _stream(x))
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    rc = lib().ssd_adapter_linear_bwd(shape, x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scale.data_ptr(), plan.buffer.data_ptr(),
+                                      dout.data_ptr(), _ptr(hidden), _ptr(dx), _ptr(da), _ptr(db), workspace.data_ptr(), workspace.numel(), flags,
+                                      _stream(x))
     if rc != 0:
         raise SSDError(rc, "ssd_adapter_linear_bwd")
     return {"dx": dx, "da": da, "db": db}
