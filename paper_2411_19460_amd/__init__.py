@@ -9,8 +9,8 @@ from .binding import (SSD_BF16, SSD_F32, SSD_FLAG_ACCUM_PARAM, SSD_FLAG_BF16_CHE
 
 
 def __getattr__(name):
-    # the autograd wrapper imports torch: load it on first use only
-    if name == "ssd_scan":
-        from .autograd import ssd_scan
-        return ssd_scan
+    # the autograd wrappers import torch: load them on first use only
+    if name in ("ssd_scan", "adapter_linear"):
+        from . import autograd
+        return getattr(autograd, name)
     raise AttributeError(name)

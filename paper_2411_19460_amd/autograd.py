@@ -1,4 +1,5 @@
-"""torch.autograd face of the C ABI: `ssd_scan(...)` is differentiable and keeps, between forward and
+"""torch.autograd faces of the C ABI.  `adapter_linear(...)` is a frozen projection with low-rank adapters, differentiable in its
+input and in the adapters.  `ssd_scan(...)` is differentiable and keeps, between forward and
 backward, only what MA-GC keeps (Sec. 3.2-3.3: the state entering every segment) -- the backward pass
 calls ssd_bwd, which restores each segment from its checkpoint.  Argument marshalling only: every
 step of the computation runs in libssd_magc.so."""
@@ -38,3 +39,28 @@ def ssd_scan(x, dt, A, B, C, D, chunk, segment=None, init_state=None, flags=0, s
     sequence is one segment).  seq_reset [Bt, L] uint8 marks the first token of every packed sequence.
     Tensors as in ssd_fwd (contiguous device tensors; dt already positive)."""
     return _SSDScan.apply(x, dt, A, B, C, D, init_state, chunk, segment, flags, seq_reset)
+
+
+class _AdapterLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, a, b, scale, plan):
+        f = binding.ssd_adapter_linear_fwd(x, w, a, b, scale, plan, want_hidden=ctx.needs_input_grad[2] or ctx.needs_input_grad[3])
+        hidden = f["hidden"]
+        ctx.save_for_backward(x, w, a, b, scale, hidden if hidden is not None else scale.new_empty(0))
+        ctx.cfg = (plan, hidden is not None)
+        return f["out"]
+
+    @staticmethod
+    def backward(ctx, dout):
+        x, w, a, b, scale, hidden = ctx.saved_tensors
+        plan, has_hidden = ctx.cfg
+        dab = ctx.needs_input_grad[2] or ctx.needs_input_grad[3]
+        g = binding.ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout.contiguous(), hidden if has_hidden else None,
+                                           want_dx=ctx.needs_input_grad[0], want_dab=dab)
+        return g["dx"], None, g["da"] if ctx.needs_input_grad[2] else None, g["db"] if ctx.needs_input_grad[3] else None, None, None
+
+
+def adapter_linear(x, w, a, b, scale, plan):
+    """x [rows, in_dim] @ w^T plus each row's low-rank adapter (see ssd_adapter_linear_fwd); differentiable in x, a and b, w frozen.
+    Autograd rounds the adapters' fp32 gradients to a's and b's bf16; ssd_adapter_linear_bwd hands them out as they are."""
+    return _AdapterLinear.apply(x, w, a, b, scale, plan)
