@@ -15,7 +15,6 @@ template <int MT, int NT, int UB = 1>
 static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], const LowRankTerm& lr, int m0, int M, int n0, int N, int lane, int u0, int ustep) {
     using namespace mf;
     const int tile = m0 / LOW_TILE, nu = lr.tile_n[2 * tile], a0 = lr.tile_n[2 * tile + 1], q = lane >> 4, l16 = lane & 15;
-    if (u0 >= nu) return;
     const int* list = lr.tile_a + (int64_t)tile * LOW_TILE;
     int of_row[MT];
 #pragma unroll
@@ -23,19 +22,21 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
         const int m = m0 + 16 * i + l16;
         of_row[i] = m < M ? lr.ids[m] : -1;
     }
+    if (u0 >= nu) return;
+    // What does not exist is fetched from beyond a descriptor's end: zeros.
+    constexpr uint32_t OUT = 0x80000000u;
+    const int rows = M - m0 < 16 * MT ? M - m0 : 16 * MT;
+    const rsrc_t rl = make_rows(lr.low + (int64_t)m0 * lr.rank, rows < 0 ? 0 : rows, lr.rank * 4);
     for (int k0 = 0; k0 < lr.rank; k0 += 32) {
         const int k = k0 + 8 * q;
-        const bool in = k < lr.rank;
+        const uint32_t kb = k < lr.rank ? (uint32_t)k : OUT;
         bf16x8 a[MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            a[i] = (bf16x8)((__bf16)0.f);
-            if (in && of_row[i] >= 0) {
-                const f32x4* p = (const f32x4*)(lr.low + (int64_t)(m0 + 16 * i + l16) * lr.rank + k);
-                const f32x4 p0 = p[0], p1 = p[1];
+        for (int i = 0; i < MT; ++i) {  // (rows without an adapter have zeros; nothing here waits for the rows' adapters)
+            const uint32_t at = ((16 * i + l16) * lr.rank + kb) * 4;
+            const f32x4 p0 = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at)), p1 = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at + 16));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) a[i][e] = (__bf16)p0[e], a[i][4 + e] = (__bf16)p1[e];
-            }
+            for (int e = 0; e < 4; ++e) a[i][e] = (__bf16)p0[e], a[i][4 + e] = (__bf16)p1[e];
         }
         for (int u = u0; u < nu; u += UB * ustep) {
             int ad[UB];
@@ -49,13 +50,12 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
             }
             bf16x8 b[UB][NT];
 #pragma unroll
-            for (int v = 0; v < UB; ++v)
+            for (int v = 0; v < UB; ++v) {
+                const int own = UB == 1 || ad[v] >= 0 ? N - n0 < 16 * NT ? N - n0 : 16 * NT : 0;  // columns that exist
+                const rsrc_t ru = make_rows(lr.up + ((int64_t)(ad[v] < 0 ? 0 : ad[v]) * lr.width + n0) * lr.rank, own < 0 ? 0 : own, lr.rank * 2);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const int n = n0 + 16 * j + l16;
-                    b[v][j] = (bf16x8)((__bf16)0.f);
-                    if (in && n < N && (UB == 1 || ad[v] >= 0)) b[v][j] = *(const bf16x8*)(lr.up + ((int64_t)ad[v] * lr.width + n) * lr.rank + k);
-                }
+                for (int j = 0; j < NT; ++j) b[v][j] = rows_load(ru, kb == OUT ? OUT : ((16 * j + l16) * lr.rank + kb) * 2);
+            }
 #pragma unroll
             for (int v = 0; v < UB; ++v)
 #pragma unroll
