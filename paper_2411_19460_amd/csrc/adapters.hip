@@ -59,7 +59,7 @@ Plan plan_of(int64_t rows, int32_t n) {
     p.first_slot = take(n + 1);   // partial sums of the gradients: adapters of several long units
     p.short_u = take(4 * (int64_t)p.max_short);
     p.long_u = take(4 * (int64_t)p.max_long);
-    p.tile_n = take(2 * (int64_t)p.tiles);
+    p.tile_n = take(p.tiles);
     p.tile_a = take((int64_t)p.tiles * LOW_TILE);
     p.counts = take(n + 1);
     p.words = at;
@@ -102,8 +102,7 @@ __global__ __launch_bounds__(PTHR) void k_plan_count(Plan p, const int* row_adap
         for (int j = 0; j < LOW_TILE; ++j) place += lds[j] < a;
         if (first) plan[p.tile_a + (int64_t)blockIdx.x * LOW_TILE + place] = a;
         const int listed = block_sum(first, lds);
-        if (tid == 0) plan[p.tile_n + 2 * blockIdx.x] = listed;
-        if (first && place == 0) plan[p.tile_n + 2 * blockIdx.x + 1] = a;
+        if (tid == 0) plan[p.tile_n + blockIdx.x] = listed;
         return;
     }
     const int mine = blockIdx.x - p.tiles;
@@ -378,8 +377,11 @@ hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, co
 
 template <bool KROW>
 hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* plan, const TurnJob& tj, hipStream_t st) {
-    // few units: a workgroup for every sixteen ranks, x fetched again
-    if (lp.rank <= 16 || p.max_short * ((lp.rank + 15) / 16) <= 256) return launch_low_rt<1, KROW>(lp, p, plan, tj, st);
+    // Few units: a workgroup for every sixteen ranks, x fetched again for the others (64 rows 5120 -> 2560 rank 32: 9.7 -> 6.7 us with
+    // sixteen instead of all thirty-two).  Where ranks are what lies side by side (KROW) thirty-two, half a cache line: 73 rows
+    // 10576 -> rank 128 34 us with sixteen.
+    if (lp.rank <= 16 || (!KROW && p.max_short * ((lp.rank + 15) / 16) <= 256)) return launch_low_rt<1, KROW>(lp, p, plan, tj, st);
+    if (KROW && p.max_short * ((lp.rank + 31) / 32) <= 256) return launch_low_rt<2, KROW>(lp, p, plan, tj, st);
     if (lp.rank <= 32) return launch_low_rt<2, KROW>(lp, p, plan, tj, st);
     return launch_low_rt<4, KROW>(lp, p, plan, tj, st);
 }

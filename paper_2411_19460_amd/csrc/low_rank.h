@@ -14,8 +14,10 @@ namespace ssdk {
 template <int MT, int NT, int UB = 1>
 static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], const LowRankTerm& lr, int m0, int M, int n0, int N, int lane, int u0, int ustep) {
     using namespace mf;
-    const int tile = m0 / LOW_TILE, nu = lr.tile_n[2 * tile], a0 = lr.tile_n[2 * tile + 1], q = lane >> 4, l16 = lane & 15;
+    const int tile = m0 / LOW_TILE, nu = lr.tile_n[tile], q = lane >> 4, l16 = lane & 15;
     const int* list = lr.tile_a + (int64_t)tile * LOW_TILE;
+    const int listed = list[lane];  // the first 64, a lane each
+    auto number = [&](int u) { return u < 64 ? __builtin_amdgcn_readlane(listed, u) : list[u]; };
     int of_row[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -27,45 +29,95 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
     constexpr uint32_t OUT = 0x80000000u;
     const int rows = M - m0 < 16 * MT ? M - m0 : 16 * MT;
     const rsrc_t rl = make_rows(lr.low + (int64_t)m0 * lr.rank, rows < 0 ? 0 : rows, lr.rank * 4);
-    for (int k0 = 0; k0 < lr.rank; k0 += 32) {
-        const int k = k0 + 8 * q;
-        const uint32_t kb = k < lr.rank ? (uint32_t)k : OUT;
-        bf16x8 a[MT];
+    struct Raw {
+        f32x4 p[MT][2];
+    };
+    auto k_of = [&](int k0) { return k0 + 8 * q < lr.rank ? (uint32_t)(k0 + 8 * q) : OUT; };  // this lane's ranks from k0 on
+    auto low_of = [&](int k0, Raw& r) {
+        const uint32_t kb = k_of(k0);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {  // (rows without an adapter have zeros; nothing here waits for the rows' adapters)
             const uint32_t at = ((16 * i + l16) * lr.rank + kb) * 4;
-            const f32x4 p0 = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at)), p1 = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at + 16));
+            r.p[i][0] = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at));
+            r.p[i][1] = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at + 16));
+        }
+    };
+    auto rounded = [&](const Raw& r, bf16x8 (&a)[MT]) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) a[i][e] = (__bf16)p0[e], a[i][4 + e] = (__bf16)p1[e];
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[i][e] = (__bf16)r.p[i][0][e], a[i][4 + e] = (__bf16)r.p[i][1][e];
+    };
+    // the operands of adapter number u of the tile (none beyond its last)
+    auto fetch = [&](int k0, int u, int& ad, bf16x8 (&b)[NT]) {
+        const uint32_t kb = k_of(k0);
+        ad = u >= nu ? -2 : number(u);
+        const int own = ad < 0 || N < n0 ? 0 : N - n0 < 16 * NT ? N - n0 : 16 * NT;  // columns that exist
+        const rsrc_t ru = make_rows(lr.up + ((int64_t)(ad < 0 ? 0 : ad) * lr.width + n0) * lr.rank, own, lr.rank * 2);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[j] = rows_load(ru, kb == OUT ? OUT : ((16 * j + l16) * lr.rank + kb) * 2);
+    };
+    auto add = [&](int ad, const bf16x8 (&a)[MT], const bf16x8 (&b)[NT]) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], (f32x4)(0.f), 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] += of_row[i] == ad ? t[e] : 0.f;
+            }
+    };
+    auto here = [&](int ad) {  // a row of this wave has it
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) any = any || of_row[i] == ad;
+        return __any(any);
+    };
+    bf16x8 a[MT];
+    if constexpr (UB == 1 && MT * NT <= 8) {
+        // Registers to spare: while an adapter's operands are multiplied those of the next (of the next ranks behind the last) are under way.
+        Raw r;
+        low_of(0, r);
+        int k0 = 0, u = u0, k1, u1, ad, ad1;
+        auto after = [&](int k, int v, int& kn, int& un) { kn = v + ustep < nu ? k : k + 32, un = v + ustep < nu ? v + ustep : u0; };
+        auto work = [&](int k, int v, int which, const bf16x8 (&b)[NT]) {
+            if (v == u0) {
+                rounded(r, a);
+                if (k + 32 < lr.rank) low_of(k + 32, r);
+            }
+            if (here(which)) add(which, a, b);
+        };
+        bf16x8 b[NT], c[NT];
+        fetch(k0, u, ad, b);
+        for (;;) {
+            after(k0, u, k1, u1);
+            if (k1 < lr.rank) fetch(k1, u1, ad1, c);
+            work(k0, u, ad, b);
+            if (k1 >= lr.rank) break;
+            after(k1, u1, k0, u);
+            if (k0 < lr.rank) fetch(k0, u, ad, b);
+            work(k1, u1, ad1, c);
+            if (k0 >= lr.rank) break;
+        }
+        return;
+    }
+    for (int k0 = 0; k0 < lr.rank; k0 += 32) {
+        {
+            Raw r;
+            low_of(k0, r);
+            rounded(r, a);
         }
         for (int u = u0; u < nu; u += UB * ustep) {
             int ad[UB];
-#pragma unroll
-            for (int v = 0; v < UB; ++v) ad[v] = u + v * ustep < nu ? u + v * ustep ? list[u + v * ustep] : a0 : -2;
             if (UB == 1) {
-                bool any = false;
-#pragma unroll
-                for (int i = 0; i < MT; ++i) any = any || of_row[i] == ad[0];
-                if (!__any(any)) continue;
+                ad[0] = number(u);
+                if (!here(ad[0])) continue;
             }
             bf16x8 b[UB][NT];
 #pragma unroll
-            for (int v = 0; v < UB; ++v) {
-                const int own = UB == 1 || ad[v] >= 0 ? N - n0 < 16 * NT ? N - n0 : 16 * NT : 0;  // columns that exist
-                const rsrc_t ru = make_rows(lr.up + ((int64_t)(ad[v] < 0 ? 0 : ad[v]) * lr.width + n0) * lr.rank, own < 0 ? 0 : own, lr.rank * 2);
+            for (int v = 0; v < UB; ++v) fetch(k0, u + v * ustep, ad[v], b[v]);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) b[v][j] = rows_load(ru, kb == OUT ? OUT : ((16 * j + l16) * lr.rank + kb) * 2);
-            }
-#pragma unroll
-            for (int v = 0; v < UB; ++v)
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[v][j], a[i], (f32x4)(0.f), 0, 0, 0);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][e] += of_row[i] == ad[v] ? t[e] : 0.f;
-                    }
+            for (int v = 0; v < UB; ++v) add(ad[v], a, b[v]);
         }
     }
 }

@@ -351,7 +351,7 @@ SideStream* side_stream();
 constexpr int LOW_TILE = 256;
 struct LowRankTerm {
     const int* ids;     // [rows]
-    const int* tile_n;  // [tiles][2]: how many adapters, the first
+    const int* tile_n;  // [tiles]: how many adapters
     const int* tile_a;  // [tiles][LOW_TILE]: which, ascending
     const float* low;   // [rows, rank]
     const bf16_t* up;   // [adapters][width][rank]
