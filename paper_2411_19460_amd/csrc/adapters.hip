@@ -9,6 +9,7 @@
 
 #include <type_traits>
 
+#include "low_rank.h"
 #include "mfma_common.h"
 
 namespace ssdk {
@@ -184,7 +185,8 @@ struct LowParams {
     int64_t ldx;
     const __bf16* u;
     const float* scale;
-    float* low;
+    float* low;      // [rows, rank], or null
+    __bf16* packed;  // the same for the wide product (packed_low), or null
     int K, rank;
 };
 constexpr int LWAVES = 8;
@@ -312,36 +314,41 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
 #pragma unroll
         for (int u = 0; u < LWAVES; ++u) o += *(const f32x4*)(sums + (u * SHORT_UNIT + r) * 16 * RT + c);
         const int64_t at = un.row0 < 0 ? perm[un.first + r] : un.row0 + r;
-        *(f32x4*)(lp.low + at * lp.rank + r0 + c) = o * s;
+        o *= s;
+        if (lp.low) *(f32x4*)(lp.low + at * lp.rank + r0 + c) = o;
+        if (lp.packed) *(bf16x4*)(lp.packed + packed_low(at, r0 + c, lp.rank)) = __builtin_convertvector(o, bf16x4);
     }
 }
 
-// a [adapters][rank][in_dim] with the rank contiguous, for the product that joins dx (see add_low_rank): pieces of 64 columns of an
-// adapter, eight ranks at a time.
-struct TurnJob {
-    const __bf16* a;
-    __bf16* to;   // [adapters][in_dim][rank]; null: no such job
-    int in_dim, rank, blocks;  // blocks: of 64 columns, times adapters
+// The adapters' other factor packed for the wide product (see LowRankTerm): pieces of 64 columns of an adapter, eight ranks at a time.
+struct PackJob {
+    const __bf16* from;  // [adapters][width][rank], or (KROW) [adapters][rank][width]
+    __bf16* to;
+    int width, rank, blocks;  // blocks: of 64 columns, times adapters; 0: no such job
 };
-__device__ __forceinline__ void turn_piece(const TurnJob& tj, const Plan& p, const int* plan, int id) {
-    const int per = (tj.in_dim + 63) / 64, a = id / per, c = (id - a * per) * 64 + (threadIdx.x & 63);
-    if (plan[p.start + a] == plan[p.start + a + 1] || c >= tj.in_dim) return;  // nobody has it
-    for (int r = 8 * (threadIdx.x >> 6); r < tj.rank; r += 8 * LWAVES) {
+template <bool KROW>
+__device__ __forceinline__ void pack_piece(const PackJob& pj, const Plan& p, const int* plan, int id) {
+    const int per = (pj.width + 63) / 64, a = id / per, c = (id - a * per) * 64 + (KROW ? threadIdx.x & 63 : threadIdx.x >> 3);
+    if (plan[p.start + a] == plan[p.start + a + 1] || c >= pj.width) return;  // nobody has it
+    __bf16* to = pj.to + (int64_t)a * ((pj.width + 15) & ~15) * pj.rank;
+    for (int r = 8 * (KROW ? threadIdx.x >> 6 : threadIdx.x & 7); r < pj.rank; r += 64) {
         bf16x8 v;
+        if (KROW)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = tj.a[((int64_t)a * tj.rank + r + e) * tj.in_dim + c];
-        *(bf16x8*)(tj.to + ((int64_t)a * tj.in_dim + c) * tj.rank + r) = v;
+            for (int e = 0; e < 8; ++e) v[e] = pj.from[((int64_t)a * pj.rank + r + e) * pj.width + c];
+        else v = *(const bf16x8*)(pj.from + ((int64_t)a * pj.width + c) * pj.rank + r);
+        *(bf16x8*)(to + packed_low(c, r, pj.rank)) = v;
     }
 }
 
 template <int RT, bool KROW>
-__global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, const int* plan, TurnJob tj) {
+__global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, const int* plan, PackJob pj) {
     extern __shared__ __attribute__((aligned(16))) char low_lds_mem[];
-    if (KROW && (int)blockIdx.x < tj.blocks) {
-        if (blockIdx.y == 0) turn_piece(tj, p, plan, blockIdx.x);
+    if ((int)blockIdx.x < pj.blocks) {
+        if (blockIdx.y == 0) pack_piece<KROW>(pj, p, plan, blockIdx.x);
         return;
     }
-    const int u = blockIdx.x - (KROW ? tj.blocks : 0);
+    const int u = blockIdx.x - pj.blocks;
     const Unit un = ((const Unit*)(plan + p.short_u))[u];
     const int r0 = blockIdx.y * 16 * RT;
     const int* perm = plan + p.perm;
@@ -350,7 +357,8 @@ __global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, co
         const int nr = lp.rank - r0 < 16 * RT ? lp.rank - r0 : 16 * RT;
         for (int v = threadIdx.x; v < un.count * nr; v += 64 * LWAVES) {
             const int64_t row = un.row0 < 0 ? perm[un.first + v / nr] : un.row0 + v / nr;
-            lp.low[row * lp.rank + r0 + v % nr] = 0.f;
+            if (lp.low) lp.low[row * lp.rank + r0 + v % nr] = 0.f;
+            if (lp.packed) lp.packed[packed_low(row, r0 + v % nr, lp.rank)] = (__bf16)0.f;
         }
         return;
     }
@@ -359,7 +367,7 @@ __global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, co
 }
 
 template <int RT, bool KROW>
-hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, const TurnJob& tj, hipStream_t st) {
+hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, const PackJob& pj, hipStream_t st) {
     constexpr int LDS = low_lds<RT, KROW>();
     static bool raised[64];
     if (LDS > 65536) {
@@ -371,19 +379,19 @@ hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, co
             raised[dev] = true;
         }
     }
-    hipLaunchKernelGGL((k_low<RT, KROW>), dim3(p.max_short + tj.blocks, (lp.rank + 16 * RT - 1) / (16 * RT)), dim3(64 * LWAVES), LDS, st, lp, p, plan, tj);
+    hipLaunchKernelGGL((k_low<RT, KROW>), dim3(p.max_short + pj.blocks, (lp.rank + 16 * RT - 1) / (16 * RT)), dim3(64 * LWAVES), LDS, st, lp, p, plan, pj);
     return hipGetLastError();
 }
 
 template <bool KROW>
-hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* plan, const TurnJob& tj, hipStream_t st) {
+hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* plan, const PackJob& pj, hipStream_t st) {
     // Few units: a workgroup for every sixteen ranks, x fetched again for the others (64 rows 5120 -> 2560 rank 32: 9.7 -> 6.7 us with
     // sixteen instead of all thirty-two).  Where ranks are what lies side by side (KROW) thirty-two, half a cache line: 73 rows
     // 10576 -> rank 128 34 us with sixteen.
-    if (lp.rank <= 16 || (!KROW && p.max_short * ((lp.rank + 15) / 16) <= 256)) return launch_low_rt<1, KROW>(lp, p, plan, tj, st);
-    if (KROW && p.max_short * ((lp.rank + 31) / 32) <= 256) return launch_low_rt<2, KROW>(lp, p, plan, tj, st);
-    if (lp.rank <= 32) return launch_low_rt<2, KROW>(lp, p, plan, tj, st);
-    return launch_low_rt<4, KROW>(lp, p, plan, tj, st);
+    if (lp.rank <= 16 || (!KROW && p.max_short * ((lp.rank + 15) / 16) <= 256)) return launch_low_rt<1, KROW>(lp, p, plan, pj, st);
+    if (KROW && p.max_short * ((lp.rank + 31) / 32) <= 256) return launch_low_rt<2, KROW>(lp, p, plan, pj, st);
+    if (lp.rank <= 32) return launch_low_rt<2, KROW>(lp, p, plan, pj, st);
+    return launch_low_rt<4, KROW>(lp, p, plan, pj, st);
 }
 
 // ---- the adapters' gradients ----
@@ -551,7 +559,17 @@ int check_shape(const ssd_adapter_shape_t* s) {
 
 size_t pad(size_t b) { return (b + 255) / 256 * 256; }
 size_t low_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->rows * s->rank * sizeof(float)); }
-size_t turned_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->nadapters * s->rank * s->in_dim * 2); }
+size_t packed_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)(s->rows + 15) / 16 * 16 * s->rank * 2); }
+size_t factor_bytes(const ssd_adapter_shape_t* s, int width) { return pad((size_t)s->nadapters * s->rank * ((width + 15) & ~15) * 2); }
+// Whether the forward product takes b packed, which costs the narrow one a pass over it.  8192 rows 2560 -> 10576 rank 64: the call 384 ->
+// 378 us; 7116 rows 1024 -> 4384 rank 16: the narrow product 6.0 -> 8.7, the wide one the same.
+bool packs_b(const ssd_adapter_shape_t* s) { return s->rows >= 2048 && s->rank > 32; }
+PackJob pack_of(const ssd_adapter_shape_t* s, const void* from, void* to, int width) {
+    return {(const __bf16*)from, (__bf16*)to, width, s->rank, s->nadapters * ((width + 63) / 64)};
+}
+LowRankTerm term_of(const Plan& p, const int* plan, const void* low, const void* up, bool packed, const ssd_adapter_shape_t* s, int width) {
+    return {plan + p.ids, plan + p.tile_n, plan + p.tile_a, (const bf16_t*)low, (const bf16_t*)up, s->rank, packed ? (width + 15) & ~15 : width, packed};
+}
 size_t part_bytes(const Plan& p, const ssd_adapter_shape_t* s, int cols) { return pad((size_t)most_slots(p) * s->rank * cols * sizeof(float)); }
 
 LowProduct product_of(const ssd_adapter_shape_t* s, bool input_grad, const void* x, const void* w, void* out) {
@@ -595,10 +613,10 @@ extern "C" int ssd_adapter_plan(int64_t rows, int32_t nadapters, const int32_t* 
 
 extern "C" size_t ssd_adapter_workspace_bytes(const ssd_adapter_shape_t* shape, int32_t is_backward) {
     if (check_shape(shape) != SSD_OK || shape->rows > SSD_MAX_ADAPTER_ROWS) return 0;
-    if (!is_backward) return low_bytes(shape) + slice_bytes(shape, false) + 256;
+    if (!is_backward) return packed_bytes(shape) + (packs_b(shape) ? factor_bytes(shape, shape->out_dim) : 0) + slice_bytes(shape, false) + 256;
     const Plan p = plan_of(shape->rows, shape->nadapters);
     const size_t slices = slice_bytes(shape, true), parts = part_bytes(p, shape, shape->in_dim) + part_bytes(p, shape, shape->out_dim);
-    return 2 * low_bytes(shape) + turned_bytes(shape) + (slices > parts ? slices : parts) + 256;  // (one is read before the other is written)
+    return 2 * low_bytes(shape) + packed_bytes(shape) + factor_bytes(shape, shape->in_dim) + (slices > parts ? slices : parts) + 256;  // (one is read before the other is written)
 }
 
 extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const void* x, const void* w, const void* a, const void* b,
@@ -614,12 +632,18 @@ extern "C" int ssd_adapter_linear_fwd(const ssd_adapter_shape_t* shape, const vo
     hipStream_t st = (hipStream_t)hip_stream;
     const Plan p = plan_of(shape->rows, shape->nadapters);
     const int* pl = (const int*)plan;
-    float* low = hidden ? hidden : (float*)workspace;
+    __bf16* packed = (__bf16*)workspace;
+    char *b_packed = (char*)workspace + packed_bytes(shape), *slices = b_packed;
+    PackJob pj = {};
+    if (packs_b(shape)) {
+        pj = pack_of(shape, b, b_packed, shape->out_dim);
+        slices += factor_bytes(shape, shape->out_dim);
+    }
     const int64_t ldx = shape->x_row_stride ? shape->x_row_stride : shape->in_dim;
-    const LowParams lp = {(const __bf16*)x, ldx, (const __bf16*)a, scale, low, shape->in_dim, shape->rank};
-    if (launch_low_products<false>(lp, p, pl, TurnJob{}, st) != hipSuccess) return SSD_ERR_LAUNCH;
-    const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, low, (const bf16_t*)b, shape->rank, shape->out_dim};
-    const hipError_t e = launch_linear_low(product_of(shape, false, x, w, out), lr, (char*)workspace + low_bytes(shape), st);
+    const LowParams lp = {(const __bf16*)x, ldx, (const __bf16*)a, scale, hidden, packed, shape->in_dim, shape->rank};
+    if (launch_low_products<false>(lp, p, pl, pj, st) != hipSuccess) return SSD_ERR_LAUNCH;
+    const LowRankTerm lr = term_of(p, pl, packed, pj.blocks ? b_packed : b, pj.blocks != 0, shape, shape->out_dim);
+    const hipError_t e = launch_linear_low(product_of(shape, false, x, w, out), lr, slices, st);
     return e == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
 }
 
@@ -647,21 +671,19 @@ extern "C" int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const vo
     const int* pl = (const int*)plan;
     char* ws = (char*)workspace;
     float *g = (float*)ws, *own_h = (float*)(ws + low_bytes(shape));
-    __bf16* turned = (__bf16*)(ws + 2 * low_bytes(shape));
-    float *part_a = (float*)((char*)turned + turned_bytes(shape)), *part_b = (float*)((char*)part_a + part_bytes(p, shape, shape->in_dim));
+    __bf16 *packed = (__bf16*)(ws + 2 * low_bytes(shape)), *a_packed = (__bf16*)((char*)packed + packed_bytes(shape));
+    float *part_a = (float*)((char*)a_packed + factor_bytes(shape, shape->in_dim)), *part_b = (float*)((char*)part_a + part_bytes(p, shape, shape->in_dim));
     const int64_t ldx = shape->x_row_stride ? shape->x_row_stride : shape->in_dim, ldd = shape->out_row_stride ? shape->out_row_stride : shape->out_dim;
-    const LowParams lg = {(const __bf16*)dout, ldd, (const __bf16*)b, scale, g, shape->out_dim, shape->rank};
-    TurnJob tj = {};
-    if (dx) tj = {(const __bf16*)a, turned, shape->in_dim, shape->rank, shape->nadapters * ((shape->in_dim + 63) / 64)};
-    if (launch_low_products<true>(lg, p, pl, tj, st) != hipSuccess) return SSD_ERR_LAUNCH;
-    if (dx) {
-        const LowRankTerm lr = {pl + p.ids, pl + p.tile_n, pl + p.tile_a, g, (const bf16_t*)turned, shape->rank, shape->in_dim};
-        if (launch_linear_low(product_of(shape, true, dout, w, dx), lr, part_a, st) != hipSuccess) return SSD_ERR_LAUNCH;
-    }
+    const LowParams lg = {(const __bf16*)dout, ldd, (const __bf16*)b, scale, da ? g : nullptr, dx ? packed : nullptr, shape->out_dim, shape->rank};
+    PackJob pj = {};
+    if (dx) pj = pack_of(shape, a, a_packed, shape->in_dim);
+    if (launch_low_products<true>(lg, p, pl, pj, st) != hipSuccess) return SSD_ERR_LAUNCH;
+    if (dx && launch_linear_low(product_of(shape, true, dout, w, dx), term_of(p, pl, packed, a_packed, true, shape, shape->in_dim), part_a, st) != hipSuccess)
+        return SSD_ERR_LAUNCH;
     if (!da) return SSD_OK;
     if (!hidden) {
-        const LowParams lh = {(const __bf16*)x, ldx, (const __bf16*)a, scale, own_h, shape->in_dim, shape->rank};
-        if (launch_low_products<false>(lh, p, pl, TurnJob{}, st) != hipSuccess) return SSD_ERR_LAUNCH;
+        const LowParams lh = {(const __bf16*)x, ldx, (const __bf16*)a, scale, own_h, nullptr, shape->in_dim, shape->rank};
+        if (launch_low_products<false>(lh, p, pl, PackJob{}, st) != hipSuccess) return SSD_ERR_LAUNCH;
         hidden = own_h;
     }
     GradParams gp;

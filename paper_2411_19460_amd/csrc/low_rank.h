@@ -4,10 +4,13 @@
 
 namespace ssdk {
 
+// Where (row, r) of a narrow product lies for the wide one: 16 bytes a row and eight ranks, the sixteen rows of a tile side by side.
+static __device__ __forceinline__ int64_t packed_low(int64_t row, int r, int rank) { return row / 16 * 16 * rank + (r >> 3) * 128 + row % 16 * 8 + (r & 7); }
+
 // acc[i][j] += low[t, :] up_a^T for the rows t = m0 + 16 i + lane % 16 and the columns n0 + 16 j + 4 (lane / 16) + 0..3, a the adapter
 // of row t: the accumulator layout of 16 x 16 x 32 MFMAs that are issued with the columns' operand first.  The rows lie in one tile of
-// the plan (LOW_TILE).  Both operands have the rank contiguous, so a lane's eight values are one piece of memory and nothing goes
-// through LDS.  `low` is rounded to bf16: the result is, and the term is the smaller part of it.  A row keeps the products with its own
+// the plan (LOW_TILE).  Nothing goes through LDS: a lane's eight values are one piece of memory in both operands.  `low` comes in the
+// order in which lanes ask for it (packed_low), rounded to bf16: the result is, and the term is the smaller part of it.  A row keeps the products with its own
 // adapter alone, by a selection and not by zeros in `low`: an infinity in one adapter stays with the rows that have it.  Of the
 // tile's adapters this call takes numbers u0, u0 + ustep, ..., UB of them at a time: with more than one all of their operands are asked
 // for before the first is used, and none is left out for having no row here.
@@ -27,35 +30,23 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
     if (u0 >= nu) return;
     // What does not exist is fetched from beyond a descriptor's end: zeros.
     constexpr uint32_t OUT = 0x80000000u;
-    const int rows = M - m0 < 16 * MT ? M - m0 : 16 * MT;
-    const rsrc_t rl = make_rows(lr.low + (int64_t)m0 * lr.rank, rows < 0 ? 0 : rows, lr.rank * 4);
-    struct Raw {
-        f32x4 p[MT][2];
-    };
-    auto k_of = [&](int k0) { return k0 + 8 * q < lr.rank ? (uint32_t)(k0 + 8 * q) : OUT; };  // this lane's ranks from k0 on
-    auto low_of = [&](int k0, Raw& r) {
+    const int tiles = M <= m0 ? 0 : (M - m0 + 15) / 16 < MT ? (M - m0 + 15) / 16 : MT;
+    const rsrc_t rl = make_rows(lr.low + (int64_t)m0 * lr.rank, tiles, lr.rank * 32);
+    auto k_of = [&](int k0) { return k0 + 8 * q < lr.rank ? (uint32_t)(k0 / 8 + q) : OUT; };  // this lane's eight ranks from k0 on
+    auto low_of = [&](int k0, bf16x8 (&a)[MT]) {  // (rows without an adapter have zeros; nothing here waits for the rows' adapters)
         const uint32_t kb = k_of(k0);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {  // (rows without an adapter have zeros; nothing here waits for the rows' adapters)
-            const uint32_t at = ((16 * i + l16) * lr.rank + kb) * 4;
-            r.p[i][0] = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at));
-            r.p[i][1] = __builtin_bit_cast(f32x4, rows_load(rl, kb == OUT ? OUT : at + 16));
-        }
-    };
-    auto rounded = [&](const Raw& r, bf16x8 (&a)[MT]) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[i][e] = (__bf16)r.p[i][0][e], a[i][4 + e] = (__bf16)r.p[i][1][e];
+        for (int i = 0; i < MT; ++i) a[i] = rows_load(rl, kb == OUT ? OUT : i * lr.rank * 32 + kb * 256 + l16 * 16);
     };
     // the operands of adapter number u of the tile (none beyond its last)
     auto fetch = [&](int k0, int u, int& ad, bf16x8 (&b)[NT]) {
         const uint32_t kb = k_of(k0);
         ad = u >= nu ? -2 : number(u);
         const int own = ad < 0 || N < n0 ? 0 : N - n0 < 16 * NT ? N - n0 : 16 * NT;  // columns that exist
-        const rsrc_t ru = make_rows(lr.up + ((int64_t)(ad < 0 ? 0 : ad) * lr.width + n0) * lr.rank, own, lr.rank * 2);
+        const rsrc_t ru = make_rows(lr.up + ((int64_t)(ad < 0 ? 0 : ad) * lr.width + n0) * lr.rank, lr.packed ? (own + 15) & ~15 : own, lr.rank * 2);
+        const uint32_t at = lr.packed ? kb * 256 + l16 * 16 : (l16 * lr.rank + kb * 8) * 2;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) b[j] = rows_load(ru, kb == OUT ? OUT : ((16 * j + l16) * lr.rank + kb) * 2);
+        for (int j = 0; j < NT; ++j) b[j] = rows_load(ru, kb == OUT ? OUT : at + j * lr.rank * 32);
     };
     auto add = [&](int ad, const bf16x8 (&a)[MT], const bf16x8 (&b)[NT]) {
 #pragma unroll
@@ -76,13 +67,14 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
     bf16x8 a[MT];
     if constexpr (UB == 1 && MT * NT <= 8) {
         // Registers to spare: while an adapter's operands are multiplied those of the next (of the next ranks behind the last) are under way.
-        Raw r;
+        bf16x8 r[MT];
         low_of(0, r);
         int k0 = 0, u = u0, k1, u1, ad, ad1;
         auto after = [&](int k, int v, int& kn, int& un) { kn = v + ustep < nu ? k : k + 32, un = v + ustep < nu ? v + ustep : u0; };
         auto work = [&](int k, int v, int which, const bf16x8 (&b)[NT]) {
             if (v == u0) {
-                rounded(r, a);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) a[i] = r[i];
                 if (k + 32 < lr.rank) low_of(k + 32, r);
             }
             if (here(which)) add(which, a, b);
@@ -102,11 +94,7 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
         return;
     }
     for (int k0 = 0; k0 < lr.rank; k0 += 32) {
-        {
-            Raw r;
-            low_of(k0, r);
-            rounded(r, a);
-        }
+        low_of(k0, a);
         for (int u = u0; u < nu; u += UB * ustep) {
             int ad[UB];
             if (UB == 1) {

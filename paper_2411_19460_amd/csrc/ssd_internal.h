@@ -353,9 +353,10 @@ struct LowRankTerm {
     const int* ids;     // [rows]
     const int* tile_n;  // [tiles]: how many adapters
     const int* tile_a;  // [tiles][LOW_TILE]: which, ascending
-    const float* low;   // [rows, rank]
-    const bf16_t* up;   // [adapters][width][rank]
-    int rank, width;    // width: columns of the whole product
+    const bf16_t* low;  // [rows, whole sixteens][rank], see packed_low
+    const bf16_t* up;   // [adapters][width][rank]; packed: sixteen columns at a time as packed_low has rows
+    int rank, width;    // width: columns of the whole product (packed: whole sixteens)
+    int packed;
 };
 int linear_check(int64_t rows, int32_t in_dim, int32_t out_dim, int64_t ldx, int64_t ldo);  // sizes and strides, as ssd_linear_fwd
 // out = x w^T + low up^T (rows of in_dim -> out_dim), or with input_grad out = x w + low up^T (rows of out_dim -> in_dim)
