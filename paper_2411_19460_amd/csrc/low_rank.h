@@ -53,9 +53,9 @@ static __device__ __forceinline__ void add_low_rank(mf::f32x4 (&acc)[MT][NT], co
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], (f32x4)(0.f), 0, 0, 0);
+                const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] += of_row[i] == ad ? t[e] : 0.f;
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = of_row[i] == ad ? t[e] : acc[i][j][e];
             }
     };
     auto here = [&](int ad) {  // a row of this wave has it
