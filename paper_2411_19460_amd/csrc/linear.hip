@@ -469,26 +469,23 @@ __global__ __launch_bounds__(GTHR, 1) void k_gemm_low_mixed(GemmParams p1, GemmP
 }
 
 // 128 x 128 tiles for products whose 256-row tiles are too few (600 rows 1024 -> 4384 25 -> 21 us, 1000 rows 768 -> 3352 22 -> 18, narrow
-// product included; in more than one round the 256-row tiles are faster): eight waves of 64 x 32, four buffers of a K step, loaded three steps
-// ahead, one barrier a step (the waves have left step t - 1: step t + 3 may come in where it was).
+// product included; in more than one round the 256-row tiles are faster): eight waves of 64 x 64, each with half of a step's k (64 x 32 with
+// all of it reads half as much again from LDS: 2967 rows 1536 -> 768 19.2 us, 16.7 so), four buffers of a K step, loaded three steps ahead, one barrier a step (the waves have left step t - 1: step t + 3 may come in where it was).
 template <bool BK>
 struct Half {
     typedef Tile<128, true> TA;
     typedef Tile<128, BK> TB;
     static constexpr int STAGE = TA::BYTES + TB::BYTES, STAGES = 4, LOADS = TA::LOADS + TB::LOADS, LDS = STAGES * STAGE;
-    static __device__ __forceinline__ void multiply(const char* st, int wm, int wn, int lane, f32x4 (&acc)[4][2]) {
+    static __device__ __forceinline__ void multiply(const char* st, int wm, int wn, int ks, int lane, f32x4 (&acc)[4][4]) {
+        bf16x8 a[4], b[4];
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 a[4], b[2];
+        for (int j = 0; j < 4; ++j) b[j] = TB::operand(st + TA::BYTES, wn * 64 + j * 16, ks, lane);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) b[j] = TB::operand(st + TA::BYTES, wn * 32 + j * 16, ks, lane);
+        for (int i = 0; i < 4; ++i) a[i] = TA::operand(st, wm * 64 + i * 16, ks, lane);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = TA::operand(st, wm * 64 + i * 16, ks, lane);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
-        }
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
     }
 };
 
@@ -497,18 +494,18 @@ __device__ __forceinline__ void half_tile(const GemmParams& gp, int id, const Lo
     typedef Half<BK> H;
     typedef typename H::TA TA;
     typedef typename H::TB TB;
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w >> 2, wn = w & 3;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), ks = w >> 2, wm = w >> 1 & 1, wn = w & 1;
     int tm, tn;
     tile_of(gp, id, tm, tn);
     const int m0 = tm * 128, n0 = tn * 128, rows_a = gp.M - m0, rows_b = gp.N - n0;
     const bf16_t *a_org = gp.A + (int64_t)m0 * gp.lda, *b_org = BK ? gp.B + (int64_t)n0 * gp.ldb : gp.B + n0;
     const uint32_t va = TA::voff(gp.lda, rows_a, tid), vb = TB::voff(gp.ldb, rows_b, tid);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-    f32x4 acc[4][2];
+    f32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = (f32x4)(0.f);
+        for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4)(0.f);
     const int steps = gp.K / BKK;
     auto issue = [&](int t) {
         const uint32_t at = lds0 + (t % H::STAGES) * H::STAGE;
@@ -520,17 +517,17 @@ __device__ __forceinline__ void half_tile(const GemmParams& gp, int id, const Lo
     };
     static_assert(TA::LOADS == 2 && TB::LOADS == 2, "");
     for (int t = 0; t < 3 && t < steps; ++t) issue(t);
-    add_low_rank<4, 2>(acc, lr, m0 + wm * 64, gp.M, n0 + wn * 32, gp.N, lane, 0, 1);
+    add_low_rank<4, 4>(acc, lr, m0 + wm * 64, gp.M, n0 + wn * 64, gp.N, lane, ks, 2);
     wait_loads();  // see gemm_tile
     int t = 0;
     for (; t + 3 < steps; ++t) {
         wait_and_meet<2 * H::LOADS>();
         issue(t + 3);
-        H::multiply(lds + (t % H::STAGES) * H::STAGE, wm, wn, lane, acc);
+        H::multiply(lds + (t % H::STAGES) * H::STAGE, wm, wn, ks, lane, acc);
     }
     for (; t < steps; ++t) {
         wait_and_meet<0>();
-        H::multiply(lds + (t % H::STAGES) * H::STAGE, wm, wn, lane, acc);
+        H::multiply(lds + (t % H::STAGES) * H::STAGE, wm, wn, ks, lane, acc);
     }
     const int left = gp.K - steps * BKK;
     if (left) {  // through registers: k beyond the end has to read as zero
@@ -538,21 +535,37 @@ __device__ __forceinline__ void half_tile(const GemmParams& gp, int id, const Lo
         TA::load_part(a_org + (int64_t)steps * BKK, gp.lda, rows_a, left, lds, tid);
         TB::load_part(b_org + (int64_t)steps * BKK * (BK ? 1 : gp.ldb), gp.ldb, rows_b, left, lds + TA::BYTES, tid);
         __syncthreads();
-        H::multiply(lds, wm, wn, lane, acc);
+        H::multiply(lds, wm, wn, ks, lane, acc);
     }
-    const int row0 = m0 + wm * 64, col0 = n0 + wn * 32, l16 = lane & 15, q = lane >> 4;
-    __syncthreads();  // as in gemm_tile: each wave turns its own tile in a patch
-    constexpr int EPITCH = 64 + 16;
-    char* patch = lds + w * (64 * EPITCH);
+    // The two halves of k meet: each wave hands half of its rows to the other that has its tile, and finishes the other half.
+    __syncthreads();
+    const int l16 = lane & 15, q = lane >> 4, keep = ks ? 2 : 0, pair = w & 3;
+    f32x4* sums = (f32x4*)lds;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) *(bf16x4*)(patch + (i * 16 + l16) * EPITCH + (j * 16 + q * 4) * 2) = __builtin_convertvector(acc[i][j], bf16x4);
+        for (int j = 0; j < 4; ++j) sums[((pair * 2 + ks) * 8 + i * 4 + j) * 64 + lane] = ks ? acc[i][j] : acc[2 + i][j];
+    __syncthreads();
+    f32x4 o[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x4 mine = ks ? acc[2 + i][j] : acc[i][j], other = sums[((pair * 2 + (ks ^ 1)) * 8 + i * 4 + j) * 64 + lane];
+            o[i][j] = ks ? other + mine : mine + other;
+        }
+    const int row0 = m0 + wm * 64 + keep * 16, col0 = n0 + wn * 64;
+    constexpr int EPITCH = 128 + 16;  // as in gemm_tile: each wave turns its own 32 x 64 in a patch (behind the sums)
+    char* patch = lds + 8 * 8192 + w * (32 * EPITCH);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *(bf16x4*)(patch + (i * 16 + l16) * EPITCH + (j * 16 + q * 4) * 2) = __builtin_convertvector(o[i][j], bf16x4);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
-        const int v = it * 64 + lane, r = v >> 2, c = v & 3, row = row0 + r, col = col0 + c * 8;
-        const bf16x8 o = *(const bf16x8*)(patch + r * EPITCH + c * 16);
-        if (row < gp.M && col < gp.N) *(bf16x8*)((__bf16*)gp.C + (int64_t)row * gp.ldc + col) = o;
+        const int v = it * 64 + lane, r = v >> 3, c = v & 7, row = row0 + r, col = col0 + c * 8;
+        const bf16x8 x = *(const bf16x8*)(patch + r * EPITCH + c * 16);
+        if (row < gp.M && col < gp.N) *(bf16x8*)((__bf16*)gp.C + (int64_t)row * gp.ldc + col) = x;
     }
 }
 
