@@ -19,6 +19,7 @@ constexpr int THR = 256, NORM_WGS = 1024, CLIP_WGS = 2048;
 // Up to this many pieces one workgroup of SOLO_THR threads does everything: a launch less costs more than the others' bandwidth brings
 // (46 336 values 9.3 -> 7.2 us a call).
 constexpr int SOLO_PIECES = 8, SOLO_THR = 1024;
+constexpr int64_t STREAM_PIECES = 8192;  // 256 MiB of fp32 gradients
 
 // Device memory of a plan: the workgroups' sums of squares, then the pieces.
 struct Piece {
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(THR) void k_grad_sum(const double* part, int parts,
     if (threadIdx.x == 0) *sum_sq = s;
 }
 
-template <bool FROM, bool TO>
+template <bool FROM, bool TO, bool STREAM>
 __device__ __forceinline__ void scale_raw(const Raw& r, const Piece& p, float c, int tid) {
     constexpr int B = TO ? 16 : 32;
     const __amdgpu_buffer_rsrc_t dst = __builtin_amdgcn_make_buffer_rsrc(p.dst, 0, vectors(p) * B, 0x00020000);
@@ -161,23 +162,24 @@ __device__ __forceinline__ void scale_raw(const Raw& r, const Piece& p, float c,
             bf16x8 o;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = (__bf16)(f[e] * c);
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), dst, at, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), dst, at, 0, STREAM ? 2 : 0);
         } else {
             f32x4 lo, hi;
 #pragma unroll
             for (int e = 0; e < 4; ++e) lo[e] = f[e] * c, hi[e] = f[4 + e] * c;
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), dst, at, 0, 0);
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), dst, at + 16, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), dst, at, 0, STREAM ? 2 : 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), dst, at + 16, 0, STREAM ? 2 : 0);
         }
     }
 }
 __device__ __forceinline__ bool stays(const Piece& p, float c) { return p.src == p.dst && c == 1.f; }
+template <bool STREAM>
 __device__ __forceinline__ void scale(const Raw& r, const Piece& p, float c, int tid) {
     switch (p.kind & 3) {
-        case 0: scale_raw<false, false>(r, p, c, tid); break;
-        case 1: scale_raw<true, false>(r, p, c, tid); break;
-        case 2: scale_raw<false, true>(r, p, c, tid); break;
-        default: scale_raw<true, true>(r, p, c, tid);
+        case 0: scale_raw<false, false, STREAM>(r, p, c, tid); break;
+        case 1: scale_raw<true, false, STREAM>(r, p, c, tid); break;
+        case 2: scale_raw<false, true, STREAM>(r, p, c, tid); break;
+        default: scale_raw<true, true, STREAM>(r, p, c, tid);
     }
     for (int i = vectors(p) * 8 + tid; i < p.n; i += THR) {
         const float v = value(p, i) * c;
@@ -192,7 +194,9 @@ __device__ __forceinline__ float factor(double norm, float max_norm) {
 
 // The pieces in reverse: what the norm read last is still in the last-level cache.  The sum of squares is *sum_sq, or (null) that of the
 // parts.  The factor is worked out in fp64 and rounded once; a NaN in it stays one.  A gradient that is its own result and needs no
-// scaling is left alone.
+// scaling is left alone.  STREAM: results by streaming stores, which leave the last-level cache to the gradients that are still to come.
+// They pay where the gradients are more than it holds: 161 M values fp32 -> bf16 295 -> 283 us a call, 21 M fp32 43 -> 49.
+template <bool STREAM>
 __global__ __launch_bounds__(THR) void k_grad_clip(const Piece* __restrict__ pieces, int64_t count, const double* part, int parts, const double* sum_sq, float max_norm,
                                                    float* norm) {
     __shared__ double lds[4];
@@ -205,7 +209,7 @@ __global__ __launch_bounds__(THR) void k_grad_clip(const Piece* __restrict__ pie
         Raw r;
         load(r, p, threadIdx.x);
         __builtin_amdgcn_sched_barrier(0);
-        scale(r, p, c, threadIdx.x);
+        scale<STREAM>(r, p, c, threadIdx.x);
     }
 }
 
@@ -230,8 +234,8 @@ __global__ __launch_bounds__(SOLO_THR) void k_grad_solo(const Piece* __restrict_
     const double n = sqrt(s);
     const float c = factor(n, max_norm);
     if (norm && threadIdx.x == 0) *norm = (float)n;
-    if (!stays(p0, c)) scale(r0, p0, c, tid);
-    if (!stays(p1, c)) scale(r1, p1, c, tid);
+    if (!stays(p0, c)) scale<false>(r0, p0, c, tid);
+    if (!stays(p1, c)) scale<false>(r1, p1, c, tid);
 }
 static_assert(SOLO_PIECES == 2 * (SOLO_THR / THR), "");
 
@@ -319,7 +323,8 @@ extern "C" int ssd_grad_clip(void* plan, int64_t pieces, const double* sum_sq, f
         return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
     }
     if (!sum_sq) launch_squares(plan, pieces, st);
-    hipLaunchKernelGGL(k_grad_clip, dim3(wgs_of(pieces, CLIP_WGS)), dim3(THR), 0, st, (const Piece*)((Head*)plan + 1), pieces, (const double*)plan,
+    const bool stream = pieces > STREAM_PIECES;
+    hipLaunchKernelGGL(stream ? k_grad_clip<true> : k_grad_clip<false>, dim3(wgs_of(pieces, CLIP_WGS)), dim3(THR), 0, st, (const Piece*)((Head*)plan + 1), pieces, (const double*)plan,
                        (int)wgs_of(pieces, NORM_WGS), sum_sq, max_norm, norm);
     return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
 }
