@@ -633,6 +633,8 @@ def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False,
         hidden = torch.empty((rows, rank), dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a dense tensor on {dev}")
     rc = lib().ssd_adapter_linear_fwd(shape, x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scale.data_ptr(), plan.buffer.data_ptr(),
                                       out.data_ptr(), _ptr(hidden), workspace.data_ptr(), workspace.numel(), _stream(x))
     if rc != 0:
@@ -653,6 +655,8 @@ def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=T
         da, db = torch.empty(a.shape, dtype=torch.float32, device=dev), torch.empty(b.shape, dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a dense tensor on {dev}")
     rc = lib().ssd_adapter_linear_bwd(shape, x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scale.data_ptr(), plan.buffer.data_ptr(),
                                       dout.data_ptr(), _ptr(hidden), _ptr(dx), _ptr(da), _ptr(db), workspace.data_ptr(), workspace.numel(), flags,
                                       _stream(x))

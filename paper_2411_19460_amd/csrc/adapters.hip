@@ -178,8 +178,9 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
 // low[t, r] = s_a sum_k X[t, k] U_a[r, k].  A workgroup takes a short unit and 16 RT of the ranks; its eight waves share out k in steps
 // of 64 and their sums meet in LDS.  A step's rows come in as 128 contiguous bytes a row (eight rows an access) and are turned into
 // operands through LDS of the wave's own, without a barrier; fetched straight as operands (sixteen rows an access) the same loads took
-// 8192 x 2560 at rank 64 39 us.  KROW: U is stored with k as the row index ([K, rank], the output side of an adapter) and is read
-// transposed.
+// 8192 x 2560 at rank 64 39 us instead of 24.  KROW: U is stored with k as the row index ([K, rank], the output side of an adapter) and is
+// read transposed.  Bound by the rows' reading where rows are many (4096 x 10576, rank 16: 24 us, 3.6 TB/s; 16384 x 2560, rank 32: 32 us,
+// 2.6 TB/s, the packing of the other factor included), by a unit's way through k where they are few (1 row of 2560 4.6 us, 64 of 5120 6.4, 600 of 4384 10.1).
 struct LowParams {
     const __bf16* x;
     int64_t ldx;
@@ -397,7 +398,9 @@ hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* pl
 // ---- the adapters' gradients ----
 // G[r, c] = sum over the rows t of a long unit of S[t, r] X[t, c], X = x (dA, with S = g) or dout (dB, with S = h).  The contraction runs
 // over the rows of both operands, which therefore go through LDS to be read transposed.  S is fp32: three bf16 parts hold its 24 bits,
-// and each takes an MFMA (the arithmetic stays far below the reading of X).  A workgroup takes 128 columns and up to 64 ranks of a unit.
+// and each takes an MFMA (the arithmetic stays far below the reading of X).  A workgroup takes 128 columns and up to 64 ranks of a unit,
+// 64 rows a step, the next two steps' rows under way.  4096 rows of 2560 and 10576, rank 16: 27 us, 3.9 TB/s; 16384 rows of 5120 and 2560,
+// rank 32: 85 us, 3.0 TB/s (S comes again for every block of columns, and its parts are worked out again).
 // Rows beyond the unit's end are zero in both operands.
 struct GradJob {
     const __bf16* x;

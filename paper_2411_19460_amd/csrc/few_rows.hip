@@ -164,6 +164,8 @@ __device__ __forceinline__ float four_sums(const float (&a)[4]) {
 // Longer rows than the waves have pieces go by in turns (two pieces of two rows to a wave do not fit the registers: 76 to 148 bytes of
 // scratch a lane, and a step of 96 heads, whose d_inner is 6144, took 8 % longer).  STEP: with the convolution step (fo.cs).  Template
 // arguments like MODE: a branch around loads ends in a wait for them.
+// LOW: a further wave works out the low-rank term of the workgroup's columns while the others stream w (one row 2560 -> 10576, rank 16:
+// 10.7 us, 5.1 TB/s, without a term 9.9).
 template <int MODE, int R, bool STEP, bool STREAM, bool LOW = false>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(FewParams fp, FewOperands fo, int cols) {
     extern __shared__ float few_sums[];  // [columns, whole fours][R][NW], then the squares [R][NW]
@@ -367,7 +369,7 @@ typedef float f32x4v __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ int64_t packed_at(int row, int k) { return ((int64_t)(k >> 3) * 16 + row) * 8 + (k & 7); }
 
 constexpr int PIECE = 256, WPITCH = PIECE * 2 + 16;  // k per piece; bytes per LDS row of a piece of w
-constexpr int LOW_WAVES = 2;  // for a low-rank term
+constexpr int LOW_WAVES = 2;  // for a low-rank term, beside those that stream w (16 rows 2560 -> 10576, 16 adapters of rank 16: 11.9 us, without 11.0)
 constexpr int MFMA_WAVES = 12, MFMA_COLS = 16, MAX_GROUPS = 8;  // waves of a workgroup at most, columns at least
 __host__ __device__ constexpr int mfma_tiles(int ks) { return ks > 10 ? 4 : 6; }  // tiles of 16 columns at most: LDS
 // Up to eight rows leave rows of a tile free: they carry what rounding the operand x in_w to bf16 left of the live rows, and

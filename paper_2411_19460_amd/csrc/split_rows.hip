@@ -4,7 +4,8 @@
 // of 64: a wave fetches a step's rows as 128 contiguous bytes each, U steps at a time, turns them into operands through LDS of its
 // own without a barrier, and the waves' sums meet in LDS once, at the end, where they are rounded and leave.  The rows' adapters are
 // shared out as well: wave w adds numbers w, w + 8, ... of the tile's.
-// What bounds it: the operands' way from the L2 (each element of x is fetched N / (16 NT) times, each of w rows / (16 MT) times).
+// What bounds it: the operands' way from the L2 (each element of x is fetched N / (16 NT) times, each of w rows / (16 MT) times) and
+// through LDS.  64 rows 5120 -> 2560, rank 32, 24 adapters: 13.1 us (w 26 MB: 2.0 TB/s); 600 rows, input gradient of 1024 -> 4384: 21.3 us.
 #include "low_rank.h"
 #include "mfma_common.h"
 
