@@ -303,7 +303,7 @@ int ssd_linear_bwd(int64_t rows, int32_t in_dim, int32_t out_dim, const void* x,
  * Errors: SSD_ERR_NULL, SSD_ERR_SHAPE, SSD_ERR_DIVISIBILITY, SSD_ERR_ARG, SSD_ERR_WORKSPACE (workspace or plan), SSD_ERR_LAUNCH.
  */
 #define SSD_MAX_ADAPTERS 16384
-#define SSD_MAX_ADAPTER_ROWS 1073741824
+#define SSD_MAX_ADAPTER_ROWS 134217728
 typedef struct {
     int64_t rows;
     int32_t in_dim, out_dim, rank, nadapters;

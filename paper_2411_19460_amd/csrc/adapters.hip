@@ -30,7 +30,8 @@ struct Unit {
 };
 struct Plan {
     int rows, n, long_unit, max_short, max_long, tiles;
-    int64_t ids, perm, start, first_long, first_slot, short_u, long_u, tile_n, tile_a, counts, words;
+    __host__ __device__ int max_several() const { return rows / long_unit < n ? rows / long_unit : n; }  // adapters of several long units, at most
+    int64_t ids, perm, start, first_long, first_slot, several, short_u, long_u, tile_n, tile_a, counts, words;
 };
 
 int long_unit_of(int64_t rows) {  // about sixteen units where all rows share an adapter, one where rows are few
@@ -58,6 +59,7 @@ Plan plan_of(int64_t rows, int32_t n) {
     p.start = take(n + 2);        // of adapter a in perm; [n]: of the rows without one
     p.first_long = take(n + 1);
     p.first_slot = take(n + 1);   // partial sums of the gradients: adapters of several long units
+    p.several = take(p.max_several());  // those adapters, -1 behind the last
     p.short_u = take(4 * (int64_t)p.max_short);
     p.long_u = take(4 * (int64_t)p.max_long);
     p.tile_n = take(p.tiles);
@@ -122,29 +124,33 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, a = blockIdx.x;
     auto shorts = [](int c) { return (c + SHORT_UNIT - 1) / SHORT_UNIT; };
     auto longs = [&](int c) { return c ? (c + p.long_unit - 1) / p.long_unit : 1; };  // (an adapter without rows has one unit without any: its gradients are zeros)
-    int start = 0, fs = 0, fl = 0, fp = 0;
+    int start = 0, fs = 0, fl = 0, fp = 0, fm = 0;
     for (int b = tid; b < a; b += PTHR) {
         const int c = plan[p.counts + b], l = longs(c);
         start += c;
         fs += shorts(c);
         fl += l;
         fp += l > 1 ? l : 0;
+        fm += l > 1;
     }
     start = block_sum(start, lds);
     fs = block_sum(fs, lds);
     fl = block_sum(fl, lds);
     fp = block_sum(fp, lds);
+    fm = block_sum(fm, lds);
     const int mine = plan[p.counts + a], ns = shorts(mine), nl = a < p.n ? longs(mine) : 0;
     if (tid == 0) {
         plan[p.start + a] = start;
         plan[p.first_long + a] = fl;
         plan[p.first_slot + a] = fp;
+        if (nl > 1) plan[p.several + fm] = a;
         if (a == p.n) plan[p.start + a + 1] = start + mine;
     }
     Unit *su = (Unit*)(plan + p.short_u), *lu = (Unit*)(plan + p.long_u);
     if (a == p.n) {
         for (int u = fs + ns + tid; u < p.max_short; u += PTHR) su[u] = Unit{0, 0, 0, 0};
         for (int u = fl + tid; u < p.max_long; u += PTHR) lu[u] = Unit{-1, 0, 0, 0};
+        for (int u = fm + tid; u < p.max_several(); u += PTHR) plan[p.several + u] = -1;
     }
     int at = start;
     const int wanted = a < p.n ? a : -1;
@@ -321,24 +327,33 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
     }
 }
 
-// The adapters' other factor packed for the wide product (see LowRankTerm): pieces of 64 columns of an adapter, eight ranks at a time.
+// The adapters' other factor packed for the wide product (see LowRankTerm): pieces of 64 columns of an adapter, eight ranks at a time.  A
+// workgroup takes one such piece of `group` adapters, of those that have rows.
 struct PackJob {
     const __bf16* from;  // [adapters][width][rank], or (KROW) [adapters][rank][width]
     __bf16* to;
-    int width, rank, blocks;  // blocks: of 64 columns, times adapters; 0: no such job
+    int width, rank, blocks, group;  // blocks: of 64 columns, times groups of adapters; 0: no such job
 };
 template <bool KROW>
 __device__ __forceinline__ void pack_piece(const PackJob& pj, const Plan& p, const int* plan, int id) {
-    const int per = (pj.width + 63) / 64, a = id / per, c = (id - a * per) * 64 + (KROW ? threadIdx.x & 63 : threadIdx.x >> 3);
-    if (plan[p.start + a] == plan[p.start + a + 1] || c >= pj.width) return;  // nobody has it
-    __bf16* to = pj.to + (int64_t)a * ((pj.width + 15) & ~15) * pj.rank;
-    for (int r = 8 * (KROW ? threadIdx.x >> 6 : threadIdx.x & 7); r < pj.rank; r += 64) {
-        bf16x8 v;
-        if (KROW)
+    const int per = (pj.width + 63) / 64, g = id / per, c = (id - g * per) * 64 + (KROW ? threadIdx.x & 63 : threadIdx.x >> 3);
+    const int end = p.n - g * pj.group < pj.group ? p.n : (g + 1) * pj.group;
+    for (int a0 = g * pj.group; a0 < end; a0 += 64) {
+        const int mine = a0 + (threadIdx.x & 63);
+        uint64_t left = __ballot(mine < end && plan[p.start + mine] != plan[p.start + mine + 1]);
+        for (; left; left &= left - 1) {
+            const int a = a0 + __builtin_ctzll(left);
+            if (c >= pj.width) continue;
+            __bf16* to = pj.to + (int64_t)a * ((pj.width + 15) & ~15) * pj.rank;
+            for (int r = 8 * (KROW ? threadIdx.x >> 6 : threadIdx.x & 7); r < pj.rank; r += 64) {
+                bf16x8 v;
+                if (KROW)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = pj.from[((int64_t)a * pj.rank + r + e) * pj.width + c];
-        else v = *(const bf16x8*)(pj.from + ((int64_t)a * pj.width + c) * pj.rank + r);
-        *(bf16x8*)(to + packed_low(c, r, pj.rank)) = v;
+                    for (int e = 0; e < 8; ++e) v[e] = pj.from[((int64_t)a * pj.rank + r + e) * pj.width + c];
+                else v = *(const bf16x8*)(pj.from + ((int64_t)a * pj.width + c) * pj.rank + r);
+                *(bf16x8*)(to + packed_low(c, r, pj.rank)) = v;
+            }
+        }
     }
 }
 
@@ -534,9 +549,9 @@ __global__ __launch_bounds__(256) void k_adapter_grads(GradParams gp, Plan p, co
 
 // Adapters of several units: their sums in order.
 __global__ __launch_bounds__(256) void k_adapter_grads_sum(GradParams gp, Plan p, const int* plan, int blocks0) {
-    const int a = blockIdx.y;
+    const int a = plan[p.several + blockIdx.y];
+    if (a < 0) return;
     const int nl = plan[p.first_long + a + 1] - plan[p.first_long + a];
-    if (nl == 1) return;
     const GradJob& jb = gp.job[(int)blockIdx.x < blocks0 ? 0 : 1];
     const int64_t size = (int64_t)gp.rank * jb.cols;
     const int64_t i = ((int64_t)(blockIdx.x - ((int)blockIdx.x < blocks0 ? 0 : blocks0)) * 256 + threadIdx.x) * 4;
@@ -568,7 +583,9 @@ size_t factor_bytes(const ssd_adapter_shape_t* s, int width) { return pad((size_
 // 378 us; 7116 rows 1024 -> 4384 rank 16: the narrow product 6.0 -> 8.7, the wide one the same.
 bool packs_b(const ssd_adapter_shape_t* s) { return s->rows >= 2048 && s->rank > 32; }
 PackJob pack_of(const ssd_adapter_shape_t* s, const void* from, void* to, int width) {
-    return {(const __bf16*)from, (__bf16*)to, width, s->rank, s->nadapters * ((width + 63) / 64)};
+    // workgroups by the thousand, not by the number of adapters: of a large set few have rows
+    const int64_t per = (width + 63) / 64, group = (s->nadapters * per + 2047) / 2048;
+    return {(const __bf16*)from, (__bf16*)to, width, s->rank, (int)((s->nadapters + group - 1) / group * per), (int)group};
 }
 LowRankTerm term_of(const Plan& p, const int* plan, const void* low, const void* up, bool packed, const ssd_adapter_shape_t* s, int width) {
     return {plan + p.ids, plan + p.tile_n, plan + p.tile_a, (const bf16_t*)low, (const bf16_t*)up, s->rank, packed ? (width + 15) & ~15 : width, packed};
@@ -698,6 +715,6 @@ extern "C" int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const vo
     if (e != hipSuccess) return SSD_ERR_LAUNCH;
     if (!most_slots(p)) return SSD_OK;  // no adapter has several units
     const int64_t b0 = ((int64_t)gp.rank * shape->in_dim + 1023) / 1024, b1 = ((int64_t)gp.rank * shape->out_dim + 1023) / 1024;
-    hipLaunchKernelGGL(k_adapter_grads_sum, dim3((unsigned)(b0 + b1), shape->nadapters), dim3(256), 0, st, gp, p, pl, (int)b0);
+    hipLaunchKernelGGL(k_adapter_grads_sum, dim3((unsigned)(b0 + b1), p.max_several()), dim3(256), 0, st, gp, p, pl, (int)b0);
     return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH;
 }
