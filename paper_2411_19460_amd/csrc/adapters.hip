@@ -185,8 +185,8 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
 // of 64 and their sums meet in LDS.  A step's rows come in as 128 contiguous bytes a row (eight rows an access) and are turned into
 // operands through LDS of the wave's own, without a barrier; fetched straight as operands (sixteen rows an access) the same loads took
 // 8192 x 2560 at rank 64 39 us instead of 24.  KROW: U is stored with k as the row index ([K, rank], the output side of an adapter) and is
-// read transposed.  Bound by the rows' reading where rows are many (4096 x 10576, rank 16: 24 us, 3.6 TB/s; 16384 x 2560, rank 32: 32 us,
-// 2.6 TB/s, the packing of the other factor included), by a unit's way through k where they are few (1 row of 2560 4.6 us, 64 of 5120 6.4, 600 of 4384 10.1).
+// read transposed.  Bound by the rows' reading where rows are many (4096 x 10576, rank 16: 23 us, 3.8 TB/s; 16384 x 2560, rank 32: 29 us,
+// 2.9 TB/s, the packing of the other factor included), by a unit's way through k where they are few (1 row of 2560 4.6 us, 64 of 5120 6.1, 600 of 4384 7.8).
 struct LowParams {
     const __bf16* x;
     int64_t ldx;
@@ -195,6 +195,7 @@ struct LowParams {
     float* low;      // [rows, rank], or null
     __bf16* packed;  // the same for the wide product (packed_low), or null
     int K, rank;
+    bool halves;     // a workgroup for each half of a unit
 };
 constexpr int LWAVES = 8;
 
@@ -360,12 +361,18 @@ __device__ __forceinline__ void pack_piece(const PackJob& pj, const Plan& p, con
 template <int RT, bool KROW>
 __global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, const int* plan, PackJob pj) {
     extern __shared__ __attribute__((aligned(16))) char low_lds_mem[];
-    if ((int)blockIdx.x < pj.blocks) {
-        if (blockIdx.y == 0) pack_piece<KROW>(pj, p, plan, blockIdx.x);
+    const int u = blockIdx.x, units = gridDim.x - pj.blocks;
+    if (u >= units) {  // behind the units, which take longer
+        if (blockIdx.y == 0) pack_piece<KROW>(pj, p, plan, u - units);
         return;
     }
-    const int u = blockIdx.x - pj.blocks;
-    const Unit un = ((const Unit*)(plan + p.short_u))[u];
+    Unit un = ((const Unit*)(plan + p.short_u))[lp.halves ? u >> 1 : u];
+    if (lp.halves) {
+        const int skip = u & 1 ? SHORT_UNIT / 2 : 0, left = un.count - skip;
+        un.count = left < 0 ? 0 : left < SHORT_UNIT / 2 ? left : SHORT_UNIT / 2;
+        un.first += skip;
+        if (un.row0 >= 0) un.row0 += skip;
+    }
     const int r0 = blockIdx.y * 16 * RT;
     const int* perm = plan + p.perm;
     if (un.count == 0) return;
@@ -383,8 +390,11 @@ __global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, co
 }
 
 template <int RT, bool KROW>
-hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, const PackJob& pj, hipStream_t st) {
+hipError_t launch_low_rt(LowParams lp, const Plan& p, const int* plan, const PackJob& pj, hipStream_t st) {
     constexpr int LDS = low_lds<RT, KROW>();
+    // where units leave half of the 256 compute units idle: 1905 rows of 5120, rank 8, 10.2 -> 7.6 us; 600 rows of 4384 9.8 -> 7.8; with 133
+    // units (4096 rows of 2560), whose halves no longer run all at once, 8.4 -> 9.9
+    lp.halves = p.max_short * ((lp.rank + 16 * RT - 1) / (16 * RT)) <= 128;
     static bool raised[64];
     if (LDS > 65536) {
         int dev = 0;
@@ -395,7 +405,7 @@ hipError_t launch_low_rt(const LowParams& lp, const Plan& p, const int* plan, co
             raised[dev] = true;
         }
     }
-    hipLaunchKernelGGL((k_low<RT, KROW>), dim3(p.max_short + pj.blocks, (lp.rank + 16 * RT - 1) / (16 * RT)), dim3(64 * LWAVES), LDS, st, lp, p, plan, pj);
+    hipLaunchKernelGGL((k_low<RT, KROW>), dim3((lp.halves ? 2 : 1) * p.max_short + pj.blocks, (lp.rank + 16 * RT - 1) / (16 * RT)), dim3(64 * LWAVES), LDS, st, lp, p, plan, pj);
     return hipGetLastError();
 }
 
