@@ -424,7 +424,7 @@ hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* pl
 // G[r, c] = sum over the rows t of a long unit of S[t, r] X[t, c], X = x (dA, with S = g) or dout (dB, with S = h).  The contraction runs
 // over the rows of both operands, which therefore go through LDS to be read transposed.  S is fp32: three bf16 parts hold its 24 bits,
 // and each takes an MFMA (the arithmetic stays far below the reading of X).  A workgroup takes 128 columns and up to 64 ranks of a unit,
-// 64 rows a step, the next two steps' rows under way.  4096 rows of 2560 and 10576, rank 16: 27 us, 3.9 TB/s; 16384 rows of 5120 and 2560,
+// 64 rows a step, the next two steps' rows under way; in PARTS 2 halves of a larger workgroup take the steps in turn.  4096 rows of 2560 and 10576, rank 16: 27 us, 3.9 TB/s; 16384 rows of 5120 and 2560,
 // rank 32: 85 us, 3.0 TB/s (S comes again for every block of columns, and its parts are worked out again).
 // Rows beyond the unit's end are zero in both operands.
 struct GradJob {
@@ -447,19 +447,20 @@ constexpr int GCOLS = 128;
 constexpr int s_row(int rt) { return rt == 4 ? 512 : 256; }
 __device__ __forceinline__ int block_at(int k, int block) { return 32 * (block ^ ((k & 3) + ((k >> 1) & 4))); }
 
-template <int RT, bool TRANS>
+template <int RT, bool TRANS, int PARTS>
 __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& gp, const Plan& p, const int* plan, const Unit un, int u, int cb, int r0, char* lds) {
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
+    const int tid = threadIdx.x & 255, part_of = PARTS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
     const int a = un.a, cnt = un.count, fl = plan[p.first_long + a], nl = plan[p.first_long + a + 1] - fl;
     const int* perm = plan + p.perm + un.first;
     auto row = [&](int t) -> int64_t { return un.row0 < 0 ? perm[t] : un.row0 + t; };
     const int c0 = cb * GCOLS;
-    char *lx = lds, *ls = lds + 64 * 256;
-    f32x4 acc[RT][2];
+    char *lx = lds + part_of * 64 * (256 + s_row(RT)), *ls = lx + 64 * 256;
+    // Even and odd steps are summed apart where two parts could have them, so that a result's bits do not depend on how many other adapters there are.
+    constexpr int SETS = RT <= 2 && PARTS == 1 ? 2 : 1;
+    f32x4 sets[SETS][RT][2];
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[t][j] = (f32x4)(0.f);
+    for (int t = 0; t < SETS * RT * 2; ++t) sets[t / (2 * RT)][t / 2 % RT][t & 1] = (f32x4)(0.f);
+    auto& acc = sets[0];
     struct Rows {
         bf16x8 x[4];
         f32x4 s[RT];
@@ -478,7 +479,7 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
             if (t0 + t < cnt && r0 + r < gp.rank) w.s[i] = *(const f32x4*)(jb.s + row(t0 + t) * gp.rank + r0 + r);
         }
     };
-    auto use = [&](Rows& w, int next) {
+    auto use = [&](Rows& w, int next, f32x4 (&acc)[RT][2]) {
         __syncthreads();  // the operands before these have been read
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -525,11 +526,26 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
         }
     };
     Rows ra, rb;
-    load(ra, 0);
-    load(rb, 64);
-    for (int t0 = 0; t0 < cnt; t0 += 128) {
-        use(ra, t0 + 128);
-        if (t0 + 64 < cnt) use(rb, t0 + 192);
+    const int mine = 64 * part_of;  // the parts take steps in turn
+    load(ra, mine);
+    load(rb, mine + 64 * PARTS);
+    for (int t0 = 0; t0 < cnt; t0 += 128 * PARTS) {
+        use(ra, t0 + mine + 128 * PARTS, acc);
+        if (t0 + 64 * PARTS < cnt) use(rb, t0 + mine + 192 * PARTS, sets[SETS - 1]);
+    }
+    if (SETS == 2)
+#pragma unroll
+        for (int t = 0; t < 2 * RT; ++t) acc[t >> 1][t & 1] += sets[SETS - 1][t >> 1][t & 1];
+    if (PARTS == 2) {  // their sums meet
+        f32x4* sums = (f32x4*)lds;
+        __syncthreads();
+        if (part_of == 1)
+#pragma unroll
+            for (int t = 0; t < 2 * RT; ++t) sums[t * 256 + tid] = acc[t >> 1][t & 1];
+        __syncthreads();
+        if (part_of == 1) return;
+#pragma unroll
+        for (int t = 0; t < 2 * RT; ++t) acc[t >> 1][t & 1] += sums[t * 256 + tid];
     }
     // TRANS: lane -> column l16, four consecutive ranks; else lane -> rank l16, four consecutive columns
     const bool direct = nl == 1;
@@ -546,15 +562,15 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
         }
 }
 
-template <int RT>
-__global__ __launch_bounds__(256) void k_adapter_grads(GradParams gp, Plan p, const int* plan) {
-    __shared__ __attribute__((aligned(16))) char lds[64 * (256 + s_row(RT))];
+template <int RT, int PARTS>
+__global__ __launch_bounds__(256 * PARTS) void k_adapter_grads(GradParams gp, Plan p, const int* plan) {
+    __shared__ __attribute__((aligned(16))) char lds[PARTS * 64 * (256 + s_row(RT))];
     const int u = blockIdx.y;
     const Unit un = ((const Unit*)(plan + p.long_u))[u];
     if (un.a < 0) return;
     const int b = blockIdx.x, r0 = blockIdx.z * 16 * RT;
-    if (b < gp.job[0].blocks) grad_unit<RT, false>(gp.job[0], gp, p, plan, un, u, b, r0, lds);
-    else grad_unit<RT, true>(gp.job[1], gp, p, plan, un, u, b - gp.job[0].blocks, r0, lds);
+    if (b < gp.job[0].blocks) grad_unit<RT, false, PARTS>(gp.job[0], gp, p, plan, un, u, b, r0, lds);
+    else grad_unit<RT, true, PARTS>(gp.job[1], gp, p, plan, un, u, b - gp.job[0].blocks, r0, lds);
 }
 
 // Adapters of several units: their sums in order.
@@ -614,7 +630,16 @@ size_t slice_bytes(const ssd_adapter_shape_t* s, bool input_grad) {
 
 template <int RT>
 hipError_t launch_grads_rt(const GradParams& gp, const Plan& p, const int* plan, hipStream_t st) {
-    hipLaunchKernelGGL((k_adapter_grads<RT>), dim3(gp.job[0].blocks + gp.job[1].blocks, p.max_long, (gp.rank + 16 * RT - 1) / (16 * RT)), dim3(256), 0, st, gp, p, plan);
+    const dim3 grid(gp.job[0].blocks + gp.job[1].blocks, p.max_long, (gp.rank + 16 * RT - 1) / (16 * RT));
+    // Up to some two workgroups a compute unit (units without rows among them) the steps of a unit one after another are the time: two parts.
+    // 600 rows of 1024 and 4384, 129 workgroups, 14.1 -> 10.2 us; 1000 rows of one adapter, 43, 31 -> 19; 4096 rows of four, 516, 19.4 -> 14.8;
+    // 1500 rows of 2560 and 10576 at rank 32, 618, 24.5 -> 25.2; 4096 rows of these at rank 16, 1236, 28.7 -> 32.  (Ranks beyond 32: LDS.)
+    if constexpr (RT <= 2)
+        if ((int64_t)grid.x * grid.y <= 576) {
+            hipLaunchKernelGGL((k_adapter_grads<RT, 2>), grid, dim3(512), 0, st, gp, p, plan);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((k_adapter_grads<RT, 1>), grid, dim3(256), 0, st, gp, p, plan);
     return hipGetLastError();
 }
 
