@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "low_rank.h"
+#include "low_steps.h"
 #include "mfma_common.h"
 
 namespace ssdk {
@@ -21,7 +22,7 @@ using namespace mf;
 // Rows in the order of their adapters (stable; rows without one last), cut into units of rows that share one: short units for the
 // narrow products, long ones for the gradients, where a unit is what is summed before anything leaves for memory.  And for every tile
 // of the wide product the adapters that its rows have.  Words of 32 bits; host and device derive the places from (rows, adapters).
-constexpr int SHORT_UNIT = 32, MAX_RANK = 256;
+constexpr int MAX_RANK = 256;
 
 // A unit: rows perm[first .. first + count - 1] of an adapter (a == n: rows without one).  row0 >= 0: they are row0, row0 + 1, ...  One load
 // tells a workgroup all that it needs; units that a batch does not have are there with no rows.
@@ -197,8 +198,6 @@ struct LowParams {
     int K, rank;
     bool halves;     // a workgroup for each half of a unit
 };
-constexpr int LWAVES = 8;
-
 constexpr int STEP_PITCH = 144;  // bytes of a row of a step in LDS: 64 k, and sixteen rows fall into distinct banks
 template <int RT>
 constexpr int low_pitch() { return 32 * RT + 16; }
@@ -236,7 +235,7 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
     int kp[2 * RT], cp[2 * RT];
 #pragma unroll
     for (int i = 0; i < 2 * RT; ++i) {
-        kp[i] = (i * 64 + lane) / vpr;
+        kp[i] = low_piece_row(i * 64 + lane, vpr);
         cp[i] = (i * 64 + lane) - kp[i] * vpr;
     }
     f32x4 acc[RT][MT];
@@ -246,7 +245,7 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
         for (int i = 0; i < MT; ++i) acc[t][i] = (f32x4)(0.f);
     // U steps at a time: all that they need is asked for before the first is used.  WHOLE: all of their k exist; else what lies beyond K
     // comes from k = 0 and is put to zero (in both operands: an infinity there would be a NaN).
-    constexpr int U = RT == 4 ? 2 : MT == 1 ? 6 : 4;
+    constexpr int U = low_group(RT, MT);
     const bf16x8 zero = (bf16x8)((__bf16)0.f);
     auto steps = [&](int k0, auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
@@ -259,8 +258,7 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
 #pragma unroll
             for (int i = 0; i < 2 * RT; ++i) {
                 if (KROW) {
-                    const int k = ks + kp[i];
-                    uv[s][i] = *(const bf16x8*)(ua + (int64_t)(WHOLE || k < lp.K ? k : 0) * lp.rank + r0 + 8 * cp[i]);
+                    uv[s][i] = *(const bf16x8*)(ua + (int64_t)low_row_asked(ks, low_piece_asked(kp[i]), WHOLE, lp.K) * lp.rank + r0 + 8 * cp[i]);
                 } else {
                     uv[s][i] = *(const bf16x8*)(ur[i] + kc);
                 }
@@ -277,7 +275,7 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
 #pragma unroll
             for (int i = 0; i < 2 * RT; ++i) {
                 if (!KROW) *(bf16x8*)(mu + (i * 8 + r8) * STEP_PITCH + 2 * c8) = in ? uv[s][i] : zero;
-                else if (kp[i] < 64) *(bf16x8*)(mu + kp[i] * low_pitch<RT>() + 16 * cp[i]) = WHOLE || ks + kp[i] < lp.K ? uv[s][i] : zero;
+                else if (low_piece_there(kp[i])) *(bf16x8*)(mu + kp[i] * low_pitch<RT>() + 16 * cp[i]) = WHOLE || ks + kp[i] < lp.K ? uv[s][i] : zero;
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own rows: its LDS operations are done in order
 #pragma unroll
@@ -305,7 +303,7 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
         }
     };
     int k0 = 64 * w;
-    for (; k0 + 64 * (LWAVES * (U - 1) + 1) <= lp.K; k0 += 64 * LWAVES * U) steps(k0, std::true_type{});
+    for (; low_whole(k0, U, lp.K); k0 += low_advance(U)) steps(k0, std::true_type{});
     if (k0 < lp.K) steps(k0, std::false_type{});
     __syncthreads();
     // lane -> row l16 of the unit's tile i, four consecutive ranks
