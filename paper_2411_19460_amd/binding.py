@@ -439,6 +439,15 @@ def ssd_conv1d_bwd(u, w, bias, state_in, dout, dstate_out=None, want_dstate=True
     return {"du": du, "dw": dw, "dbias": dbias, "dstate_in": dstate_in}
 
 
+def _row_stride(t, name):
+    """Elements between the rows of t [rows, dim].  Rows that share memory (a broadcast row: distance 0, which the C ABI takes as dense) are
+    refused: the call would run over what the tensor does not have."""
+    rows, dim = t.shape
+    if rows > 1 and t.stride(0) < dim:
+        raise ValueError(f"the rows of {name} must not share memory (a broadcast tensor needs .contiguous())")
+    return t.stride(0) if rows > 1 else dim
+
+
 def _norm_shape(y, z, ngroups, eps, *same_as):
     """y, z: [rows, dim] with unit stride along dim (rows may be a column slice of a wider tensor)."""
     import torch
@@ -452,7 +461,7 @@ def _norm_shape(y, z, ngroups, eps, *same_as):
     if dt == SSD_F32 and y.dtype != torch.float32:
         raise TypeError("dtype must be float32 or bfloat16")
     T, C = y.shape
-    return ssd_norm_shape_t(dt, C, ngroups, eps, T, y.stride(0) if T > 1 else C, z.stride(0) if z is not None and T > 1 else C)
+    return ssd_norm_shape_t(dt, C, ngroups, eps, T, _row_stride(y, "y"), C if z is None else _row_stride(z, "z"))
 
 
 def _norm_weight(w, C):
@@ -504,7 +513,7 @@ def _rows_view(t, name):
     import torch
     if t.dim() != 2 or not t.is_cuda or t.dtype != torch.bfloat16 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be a [rows, dim] bf16 device tensor with unit stride along dim")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return _row_stride(t, name)
 
 
 def ssd_linear_fwd(x, w, out=None):
