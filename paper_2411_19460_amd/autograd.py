@@ -61,6 +61,11 @@ class _AdapterLinear(torch.autograd.Function):
 
 
 def adapter_linear(x, w, a, b, scale, plan):
-    """x [rows, in_dim] @ w^T plus each row's low-rank adapter (see ssd_adapter_linear_fwd); differentiable in x, a and b, w frozen.
+    """x [rows, in_dim] @ w^T plus each row's low-rank adapter (see ssd_adapter_linear_fwd); differentiable in x, a and b.  w and scale
+    are constants: where gradients are recorded neither may require one (w's is ssd_linear_bwd's).
     Autograd rounds the adapters' fp32 gradients to a's and b's bf16; ssd_adapter_linear_bwd hands them out as they are."""
+    if torch.is_grad_enabled():
+        for name, t in (("w", w), ("scale", scale)):
+            if t.requires_grad:
+                raise ValueError(f"{name} requires a gradient, and adapter_linear has none for it: pass {name}.detach()")
     return _AdapterLinear.apply(x, w, a, b, scale, plan)
