@@ -14,6 +14,7 @@ import math
 import time
 
 import torch
+from torch.autograd.function import once_differentiable
 
 import paper_2411_19460_amd as pk
 
@@ -29,6 +30,7 @@ class _Conv(torch.autograd.Function):
         return pk.ssd_conv1d_fwd(u, w, bias, want_state=False)[0]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         return pk.ssd_conv1d_bwd(*ctx.saved_tensors, None, dout.contiguous(), want_dstate=False)["du"], None, None
 
@@ -42,6 +44,7 @@ class _Norm(torch.autograd.Function):
         return pk.ssd_gated_norm_fwd(y, z, w)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         y, w, *z = ctx.saved_tensors
         g = pk.ssd_gated_norm_bwd(y, z[0] if z else None, w, dout.contiguous())

@@ -6,6 +6,7 @@ step of the computation runs in libssd_magc.so."""
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -21,6 +22,7 @@ class _SSDScan(torch.autograd.Function):
         return y, final
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dfinal):
         x, dt, A, B, C, D, init_state, bnd = ctx.saved_tensors
         chunk, segment, flags, has_init, has_bnd = ctx.cfg
@@ -51,6 +53,7 @@ class _AdapterLinear(torch.autograd.Function):
         return f["out"]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         x, w, a, b, scale, hidden = ctx.saved_tensors
         plan, has_hidden = ctx.cfg
@@ -63,7 +66,8 @@ class _AdapterLinear(torch.autograd.Function):
 def adapter_linear(x, w, a, b, scale, plan):
     """x [rows, in_dim] @ w^T plus each row's low-rank adapter (see ssd_adapter_linear_fwd); differentiable in x, a and b.  w and scale
     are constants: where gradients are recorded neither may require one (w's is ssd_linear_bwd's).
-    Autograd rounds the adapters' fp32 gradients to a's and b's bf16; ssd_adapter_linear_bwd hands them out as they are."""
+    A gradient of a gradient is an error.  Autograd rounds the adapters' fp32 gradients to a's and b's bf16; ssd_adapter_linear_bwd hands
+    them out as they are."""
     if torch.is_grad_enabled():
         for name, t in (("w", w), ("scale", scale)):
             if t.requires_grad:

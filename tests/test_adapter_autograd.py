@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2411_19460_amd as pk
+from paper_2411_19460_amd import binding
 
 
 def operands():
@@ -19,3 +20,31 @@ def test_constants_that_require_a_gradient(name):
     # nothing is recorded here, so nothing is lost: the call gets as far as its next check (of the plan)
     with torch.no_grad(), pytest.raises(ValueError, match="plan"):
         pk.adapter_linear(**t)
+
+
+@pytest.fixture
+def on_cpu(monkeypatch):
+    """One adapter that every row has, computed by torch in place of the C ABI's calls."""
+    def fwd(x, w, a, b, scale, plan, want_hidden=False):
+        h = scale[0] * (x.float() @ a[0].float().t())
+        return {"out": (x.float() @ w.float().t() + h @ b[0].float().t()).bfloat16(), "hidden": h if want_hidden else None}
+
+    def bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=True, want_dab=True):
+        d, x = dout.float(), x.float()
+        g = scale[0] * (d @ b[0].float())
+        h = scale[0] * (x @ a[0].float().t())
+        return {"dx": (d @ w.float() + g @ a[0].float()).bfloat16() if want_dx else None, "da": (g.t() @ x)[None] if want_dab else None,
+                "db": (d.t() @ h)[None] if want_dab else None}
+
+    monkeypatch.setattr(binding, "ssd_adapter_linear_fwd", fwd)
+    monkeypatch.setattr(binding, "ssd_adapter_linear_bwd", bwd)
+
+
+def test_a_gradient_of_a_gradient_is_an_error(on_cpu):
+    """out is bilinear in x and a: d(dx)/da is not zero, and it was taken to be."""
+    r = lambda *s: torch.randn(s, generator=torch.Generator().manual_seed(sum(s))).bfloat16()
+    x, a, b = r(4, 64).requires_grad_(), r(1, 8, 64).requires_grad_(), r(1, 72, 8).requires_grad_()
+    out = pk.adapter_linear(x, r(72, 64), a, b, torch.ones(1), None)
+    (dx,) = torch.autograd.grad(out.float().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiate twice"):
+        dx.float().square().sum().backward()
