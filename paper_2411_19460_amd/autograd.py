@@ -11,6 +11,12 @@ from torch.autograd.function import once_differentiable
 from . import binding
 
 
+def _dense(grad):
+    """What autograd hands in may be a view that begins anywhere in a larger gradient; the calls take dense tensors on 16 bytes."""
+    grad = grad.contiguous()
+    return grad if grad.data_ptr() % 16 == 0 else grad.clone()
+
+
 class _SSDScan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, dt, A, B, C, D, init_state, chunk, segment, flags, seq_reset):
@@ -58,7 +64,7 @@ class _AdapterLinear(torch.autograd.Function):
         x, w, a, b, scale, hidden = ctx.saved_tensors
         plan, has_hidden = ctx.cfg
         dab = ctx.needs_input_grad[2] or ctx.needs_input_grad[3]
-        g = binding.ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout.contiguous(), hidden if has_hidden else None,
+        g = binding.ssd_adapter_linear_bwd(x, w, a, b, scale, plan, _dense(dout), hidden if has_hidden else None,
                                            want_dx=ctx.needs_input_grad[0], want_dab=dab)
         return g["dx"], None, g["da"] if ctx.needs_input_grad[2] else None, g["db"] if ctx.needs_input_grad[3] else None, None, None
 

@@ -48,3 +48,21 @@ def test_a_gradient_of_a_gradient_is_an_error(on_cpu):
     (dx,) = torch.autograd.grad(out.float().square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="differentiate twice"):
         dx.float().square().sum().backward()
+
+
+@pytest.mark.parametrize("begin", [0, 1, 3, 8])
+def test_gradients_that_begin_anywhere(on_cpu, monkeypatch, begin):
+    """out joined with something else: its gradient is a piece of the whole one, at any element."""
+    seen, plain = [], binding.ssd_adapter_linear_bwd
+
+    def bwd(x, w, a, b, scale, plan, dout, *args, **kw):
+        seen.append((dout.data_ptr() % 16, dout.is_contiguous()))
+        return plain(x, w, a, b, scale, plan, dout, *args, **kw)
+
+    monkeypatch.setattr(binding, "ssd_adapter_linear_bwd", bwd)
+    r = lambda *s: torch.randn(s, generator=torch.Generator().manual_seed(sum(s))).bfloat16()
+    x, w, a, b, one = r(4, 64).requires_grad_(), r(72, 64), r(1, 8, 64), r(1, 72, 8), torch.ones(1)
+    dout = r(begin + 4 * 72)
+    torch.cat([torch.zeros(begin, dtype=torch.bfloat16), pk.adapter_linear(x, w, a, b, one, None).flatten()]).backward(dout)
+    assert seen == [(0, True)]
+    assert torch.equal(x.grad, plain(x, w, a, b, one, None, dout[begin:].view(4, 72))["dx"])
