@@ -654,8 +654,10 @@ def ssd_adapter_linear_fwd(x, w, a, b, scale, plan, out=None, want_hidden=False,
 def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=True, want_dab=True, flags=0, dx=None, da=None, db=None,
                            workspace=None):
     """dict(dx, da, db) for the loss <dout, out>; da and db are fp32, shaped as a and b; w is frozen (its gradient is ssd_linear_bwd's).
-    `hidden`: the forward call's, worked out again if None."""
+    `hidden`: the forward call's, worked out again if None.  SSD_FLAG_ACCUM_PARAM adds to the da and db that are given."""
     import torch
+    if flags & SSD_FLAG_ACCUM_PARAM and want_dab and da is None and db is None:
+        raise ValueError("SSD_FLAG_ACCUM_PARAM adds to da and db: both must be given")
     shape, _, nbytes = _adapter_call(plan, x, w, a, b, scale, dout, hidden, dx, da, db, 1)
     dev = x.device
     if dx is None and want_dx:

@@ -66,3 +66,10 @@ def test_gradients_that_begin_anywhere(on_cpu, monkeypatch, begin):
     torch.cat([torch.zeros(begin, dtype=torch.bfloat16), pk.adapter_linear(x, w, a, b, one, None).flatten()]).backward(dout)
     assert seen == [(0, True)]
     assert torch.equal(x.grad, plain(x, w, a, b, one, None, dout[begin:].view(4, 72))["dx"])
+
+
+def test_gradients_are_added_to_what_is_given_alone():
+    """Without da and db the sums would be added to memory that nobody has written."""
+    t = operands()
+    with pytest.raises(ValueError, match="SSD_FLAG_ACCUM_PARAM"):
+        pk.ssd_adapter_linear_bwd(**t, dout=torch.zeros((4, 72), dtype=torch.bfloat16), flags=pk.SSD_FLAG_ACCUM_PARAM)
