@@ -285,7 +285,7 @@ int ssd_linear_bwd(int64_t rows, int32_t in_dim, int32_t out_dim, const void* x,
  *     g[t,r]   = scale[a] sum_o dout[t,o] b_a[o,r]                 dx[t,i]  = sum_o dout[t,o] w[o,i] + sum_r g[t,r] a_a[r,i]
  *     da_a[r,i] = sum over a's rows of g[t,r] x[t,i]               db_a[o,r] = sum over a's rows of dout[t,o] h[t,r]
  * so that a batch may mix prompts and single tokens of requests with different adapters, and training several tasks.
- * bf16 storage, fp32 accumulation; each of out and dx is rounded once.  A row meets its own adapter's values alone: infinities
+ * bf16 storage, fp32 accumulation; each of out and dx is rounded once (h and g enter them with 16 bits, da and db with 24).  A row meets its own adapter's values alone: infinities
  * and NaN of another adapter or row do not reach it.  dw, where w is trained too, is ssd_linear_bwd's.
  *   x, out, dout, dx and w as in ssd_linear_fwd / ssd_linear_bwd (column slices allowed; out_row_stride is dout's as well)
  *   a [nadapters, rank, in_dim], b [nadapters, out_dim, rank] bf16, scale [nadapters] fp32, dense

@@ -194,7 +194,7 @@ struct LowParams {
     const __bf16* u;
     const float* scale;
     float* low;      // [rows, rank], or null
-    __bf16* packed;  // the same for the wide product (packed_low), or null
+    __bf16* packed;  // the same in two parts for the wide product (packed_low), or null
     int K, rank;
     bool halves;     // a workgroup for each half of a unit
 };
@@ -322,7 +322,17 @@ __device__ __forceinline__ void low_unit(const LowParams& lp, const int* perm, c
         const int64_t at = un.row0 < 0 ? perm[un.first + r] : un.row0 + r;
         o *= s;
         if (lp.low) *(f32x4*)(lp.low + at * lp.rank + r0 + c) = o;
-        if (lp.packed) *(bf16x4*)(lp.packed + packed_low(at, r0 + c, lp.rank)) = __builtin_convertvector(o, bf16x4);
+        if (lp.packed) {
+            bf16x4 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                __bf16 h, l;
+                split_low(o[e], h, l);
+                hi[e] = h, lo[e] = l;
+            }
+            *(bf16x4*)(lp.packed + packed_low(at, r0 + c, lp.rank, 0)) = hi;
+            *(bf16x4*)(lp.packed + packed_low(at, r0 + c, lp.rank, 1)) = lo;
+        }
     }
 }
 
@@ -350,7 +360,7 @@ __device__ __forceinline__ void pack_piece(const PackJob& pj, const Plan& p, con
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = pj.from[((int64_t)a * pj.rank + r + e) * pj.width + c];
                 else v = *(const bf16x8*)(pj.from + ((int64_t)a * pj.width + c) * pj.rank + r);
-                *(bf16x8*)(to + packed_low(c, r, pj.rank)) = v;
+                *(bf16x8*)(to + packed_up(c, r, pj.rank)) = v;
             }
         }
     }
@@ -379,7 +389,7 @@ __global__ __launch_bounds__(64 * LWAVES, 2) void k_low(LowParams lp, Plan p, co
         for (int v = threadIdx.x; v < un.count * nr; v += 64 * LWAVES) {
             const int64_t row = un.row0 < 0 ? perm[un.first + v / nr] : un.row0 + v / nr;
             if (lp.low) lp.low[row * lp.rank + r0 + v % nr] = 0.f;
-            if (lp.packed) lp.packed[packed_low(row, r0 + v % nr, lp.rank)] = (__bf16)0.f;
+            if (lp.packed) lp.packed[packed_low(row, r0 + v % nr, lp.rank, 0)] = lp.packed[packed_low(row, r0 + v % nr, lp.rank, 1)] = (__bf16)0.f;
         }
         return;
     }
@@ -601,7 +611,7 @@ int check_shape(const ssd_adapter_shape_t* s) {
 
 size_t pad(size_t b) { return (b + 255) / 256 * 256; }
 size_t low_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)s->rows * s->rank * sizeof(float)); }
-size_t packed_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)(s->rows + 15) / 16 * 16 * s->rank * 2); }
+size_t packed_bytes(const ssd_adapter_shape_t* s) { return pad((size_t)(s->rows + 15) / 16 * 16 * s->rank * 2 * 2); }  // two parts
 size_t factor_bytes(const ssd_adapter_shape_t* s, int width) { return pad((size_t)s->nadapters * s->rank * ((width + 15) & ~15) * 2); }
 // Whether the forward product takes b packed, which costs the narrow one a pass over it.  8192 rows 2560 -> 10576 rank 64: the call 384 ->
 // 378 us; 7116 rows 1024 -> 4384 rank 16: the narrow product 6.0 -> 8.7, the wide one the same.

@@ -353,8 +353,8 @@ struct LowRankTerm {
     const int* ids;     // [rows]
     const int* tile_n;  // [tiles]: how many adapters
     const int* tile_a;  // [tiles][LOW_TILE]: which, ascending
-    const bf16_t* low;  // [rows, whole sixteens][rank], see packed_low
-    const bf16_t* up;   // [adapters][width][rank]; packed: sixteen columns at a time as packed_low has rows
+    const bf16_t* low;  // [rows, whole sixteens][rank] in two parts, see packed_low
+    const bf16_t* up;   // [adapters][width][rank]; packed: sixteen columns at a time, see packed_up
     int rank, width;    // width: columns of the whole product (packed: whole sixteens)
     int packed;
 };

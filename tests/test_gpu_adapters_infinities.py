@@ -1,0 +1,39 @@
+"""An infinity in one operand, in a row or an adapter that meets it: every result is what the formula gives, infinite with its sign or NaN at
+the same places as in fp64, and unchanged (bounds of test_gpu_adapters.py) where the infinity does not come in."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_19460_amd as pk
+from oracle import adapter_ref
+from test_gpu_adapters import bounds, dev, draw, host, inside
+from test_gpu_adapters_parts import SHAPES
+
+pytestmark = pytest.mark.gpu
+
+
+def as_formula(name, got, ref, clean, off):
+    wild = ~np.isfinite(ref)
+    assert np.array_equal(got[wild], ref[wild], equal_nan=True), f"{name}: {np.sum(~((got == ref) | (np.isnan(got) & np.isnan(ref)))[wild])} of {wild.sum()} that are not finite"
+    inside(name, got[~wild], clean[~wild], off[~wild])
+
+
+@pytest.mark.parametrize("T,I,O,R", SHAPES)
+@pytest.mark.parametrize("where", ["a", "b"])
+def test_an_infinity(where, T, I, O, R):
+    n = 3
+    ops = dict(zip(("x", "w", "a", "b", "scale", "ids", "dout"), draw(T + O, T, I, O, R, n, np.arange(T) * 2 % n)))
+    clean, off = bounds(**ops)
+    t = min(T - 1, 1)
+    at = {"x": (t, I // 2), "dout": (t, O // 3), "a": (ops["ids"][t], R // 2, I // 3), "b": (ops["ids"][t], O // 2, R // 3)}[where]
+    ops[where] = ops[where].copy()
+    ops[where][at] = -np.inf if T % 2 else np.inf
+    with np.errstate(all="ignore"):
+        *most, dout = ops.values()
+        ref = {**adapter_ref.adapter_fwd(*most), **adapter_ref.adapter_bwd(*most, dout)}
+    plan = pk.ssd_adapter_plan(torch.from_numpy(ops["ids"].astype(np.int32)).cuda(), n)
+    args = (*(dev(ops[k]) for k in ("x", "w", "a", "b")), dev(ops["scale"], torch.float32), plan)
+    f = pk.ssd_adapter_linear_fwd(*args, want_hidden=True)
+    g = pk.ssd_adapter_linear_bwd(*args, dev(ops["dout"]), hidden=f["hidden"])
+    for name, got in {**f, **g}.items():
+        as_formula(name, host(got), ref[name], clean[name], off[name])
