@@ -430,8 +430,8 @@ hipError_t launch_low_products(const LowParams& lp, const Plan& p, const int* pl
 
 // ---- the adapters' gradients ----
 // G[r, c] = sum over the rows t of a long unit of S[t, r] X[t, c], X = x (dA, with S = g) or dout (dB, with S = h).  The contraction runs
-// over the rows of both operands, which therefore go through LDS to be read transposed.  S is fp32: three bf16 parts hold its 24 bits,
-// and each takes an MFMA (the arithmetic stays far below the reading of X).  A workgroup takes 128 columns and up to 64 ranks of a unit,
+// over the rows of both operands, which therefore go through LDS to be read transposed.  S is fp32: three bf16 parts of one sign (cut)
+// hold its 24 bits, and each takes an MFMA (the arithmetic stays far below the reading of X).  A workgroup takes 128 columns and up to 64 ranks of a unit,
 // 64 rows a step, the next two steps' rows under way; in PARTS 2 halves of a larger workgroup take the steps in turn.  4096 rows of 2560 and 10576, rank 16: 27 us, 3.9 TB/s; 16384 rows of 5120 and 2560,
 // rank 32: 85 us, 3.0 TB/s (S comes again for every block of columns, and its parts are worked out again).
 // Rows beyond the unit's end are zero in both operands.
@@ -499,9 +499,13 @@ __device__ __forceinline__ void grad_unit(const GradJob& jb, const GradParams& g
             const int v = i * 256 + tid, t = v / (4 * RT), r = 4 * (v % (4 * RT));
 #pragma unroll
             for (int part = 0; part < 3; ++part) {
-                const bf16x4 b = __builtin_convertvector(w.s[i], bf16x4);
+                bf16x4 b;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w.s[i][e] = __builtin_isinf((float)b[e]) ? 0.f : w.s[i][e] - (float)b[e];  // (an infinity: the first part alone)
+                for (int e = 0; e < 4; ++e) {
+                    float v = w.s[i][e];
+                    b[e] = cut(v);
+                    w.s[i][e] = v;
+                }
                 *(bf16x4*)(ls + t * s_row(RT) + block_at(t, part * RT + (r >> 4)) + 2 * (r & 15)) = b;
             }
         }

@@ -11,13 +11,17 @@ static __device__ __forceinline__ int64_t packed_low(int64_t row, int r, int ran
     return (row / 16 * 2 + part) * 16 * rank + (r >> 3) * 128 + row % 16 * 8 + (r & 7);
 }
 
-// v in two bf16 parts, 16 bits of it or more.  The first is cut off, not rounded, so that the second has its sign, and where nothing is left the
-// second is 2^-30 of v instead of zero: times an infinity of the other operand both parts are the infinity that v would be (a zero, or a
-// part of the other sign, would make a NaN of it).  An infinity's second part is itself, a NaN's a NaN.
-static __device__ __forceinline__ void split_low(float v, __bf16& hi, __bf16& lo) {
+// The next bf16 part of v, which keeps the rest.  Parts are cut off, not rounded, so that they have one sign, and where nothing is left the
+// rest is 2^-30 of v instead of zero: times an infinity of the other operand all parts are the infinity that v would be (a zero, or a part
+// of the other sign, would make a NaN of it).  An infinity's rest is itself, a NaN's a NaN.
+static __device__ __forceinline__ __bf16 cut(float& v) {
     const float top = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xffff0000u);
-    hi = (__bf16)top;
-    lo = (__bf16)(top == v ? v * 0x1p-30f : v - top);
+    v = top == v ? v * 0x1p-30f : v - top;
+    return (__bf16)top;
+}
+static __device__ __forceinline__ void split_low(float v, __bf16& hi, __bf16& lo) {  // 16 bits of v or more
+    hi = cut(v);
+    lo = (__bf16)v;
 }
 
 // acc[i][j] += low[t, :] up_a^T for the rows t = m0 + 16 i + lane % 16 and the columns n0 + 16 j + 4 (lane / 16) + 0..3, a the adapter

@@ -19,7 +19,7 @@ def as_formula(name, got, ref, clean, off):
 
 
 @pytest.mark.parametrize("T,I,O,R", SHAPES)
-@pytest.mark.parametrize("where", ["a", "b"])
+@pytest.mark.parametrize("where", ["x", "dout", "a", "b"])
 def test_an_infinity(where, T, I, O, R):
     n = 3
     ops = dict(zip(("x", "w", "a", "b", "scale", "ids", "dout"), draw(T + O, T, I, O, R, n, np.arange(T) * 2 % n)))
