@@ -333,7 +333,8 @@ int ssd_adapter_linear_bwd(const ssd_adapter_shape_t* shape, const void* x, cons
  *           device) = sqrt(S), or NULL.  A gradient that is its own result is
  *           left alone where the factor is 1.  Non-finite gradients act as the formula says: an infinite norm gives a factor of 0
  *           (and NaN where 0 meets an infinity), a NaN makes everything NaN; the norm tells a caller to drop the step.
- * max_norm >= 0, infinity for the norm alone.  Everything is enqueued on hip_stream, nothing is allocated, the host does not wait.
+ * max_norm >= 0; infinity is no bound: the factor is 1 whatever the norm, also an infinite one or a NaN (the norm alone, gradients in place
+ * are left as they are).  Everything is enqueued on hip_stream, nothing is allocated, the host does not wait.
  * Errors: SSD_ERR_NULL, SSD_ERR_SHAPE, SSD_ERR_DTYPE, SSD_ERR_ARG, SSD_ERR_WORKSPACE, SSD_ERR_LAUNCH.
  */
 typedef struct {

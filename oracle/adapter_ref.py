@@ -40,5 +40,5 @@ def clip(grads, max_norm):
     with np.errstate(all="ignore"):
         norm = np.sqrt(np.float64(sum(float(np.sum(np.square(g))) for g in grads)))
         by = np.float64(max_norm) / (norm + 1e-6)
-        by = by if not by > 1.0 else 1.0
+        by = by if not by > 1.0 and max_norm < np.inf else 1.0     # an infinite max_norm is no bound, also where the norm is not finite
         return norm, [g * by for g in grads]

@@ -724,7 +724,8 @@ def _check_sum_sq(sum_sq, plan):
 
 
 def ssd_grad_clip(plan: GradPlan, max_norm: float, sum_sq=None):
-    """Scales the plan's gradients by min(1, max_norm / (norm + 1e-6)) into its results and returns norm [1] fp32.  sum_sq: the sum of
+    """Scales the plan's gradients by min(1, max_norm / (norm + 1e-6)) into its results and returns norm [1] fp32; an infinite max_norm
+    scales nothing, whatever the norm.  sum_sq: the sum of
     squares that the norm is the root of (None: the plan's own)."""
     import torch
     if not max_norm >= 0:

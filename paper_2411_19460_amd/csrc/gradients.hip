@@ -188,6 +188,7 @@ __device__ __forceinline__ void scale(const Raw& r, const Piece& p, float c, int
     }
 }
 __device__ __forceinline__ float factor(double norm, float max_norm) {
+    if (max_norm == __builtin_inff()) return 1.f;  // no bound: infinite or not a number, the norm is all that is asked for
     const double by = (double)max_norm / (norm + 1e-6);
     return by > 1.0 ? 1.f : (float)by;
 }
