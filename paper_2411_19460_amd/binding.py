@@ -677,10 +677,13 @@ def ssd_adapter_linear_bwd(x, w, a, b, scale, plan, dout, hidden=None, want_dx=T
 
 
 class GradPlan:
-    """The pieces of a list of gradients (ssd_grad_plan).  It keeps the tensors alive whose addresses it holds."""
+    """The pieces of a list of gradients (ssd_grad_plan): the memory that the tensors had when it was made, which it keeps alive.  A tensor that
+    is given other memory afterwards (t.data = ..., t.set_) needs a new plan."""
 
     def __init__(self, buffer, pieces: int, grads, outs):
         self.buffer, self.pieces, self.grads, self.outs = buffer, pieces, grads, outs
+        # the memory itself: the tensors alone would let go of it with their next assignment to .data
+        self._memory = [t.untyped_storage() for t in (grads if outs is grads else (*grads, *outs))]
 
 
 def ssd_grad_plan(grads, outs=None) -> GradPlan:
