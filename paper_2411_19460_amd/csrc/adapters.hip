@@ -4,7 +4,8 @@
 //     dA_a = sum_{t of a} g[t, :]^T x[t, :]  dB_a = sum_{t of a} dout[t, :]^T h[t, :]
 // with the projection W frozen.  The products with W and the low-rank terms that join them are tiles of linear.hip; here are the plan
 // of a batch (which rows share an adapter), the narrow products h and g, and the adapters' gradients.
-// h and g are fp32, and so is everything that is summed: the gradients leave in fp32, and would lose 16 of its bits with either in bf16.
+// h and g are fp32, and so is everything that is summed: the gradients leave in fp32, and would lose 16 of its bits with either in bf16.  For the
+// wide products, whose results are bf16, they come in two bf16 parts.
 #include <string.h>
 
 #include <type_traits>
@@ -186,8 +187,8 @@ __global__ __launch_bounds__(PTHR) void k_plan_rows(Plan p, int* plan) {
 // of 64 and their sums meet in LDS.  A step's rows come in as 128 contiguous bytes a row (eight rows an access) and are turned into
 // operands through LDS of the wave's own, without a barrier; fetched straight as operands (sixteen rows an access) the same loads took
 // 8192 x 2560 at rank 64 39 us instead of 24.  KROW: U is stored with k as the row index ([K, rank], the output side of an adapter) and is
-// read transposed.  Bound by the rows' reading where rows are many (4096 x 10576, rank 16: 23 us, 3.8 TB/s; 16384 x 2560, rank 32: 29 us,
-// 2.9 TB/s, the packing of the other factor included), by a unit's way through k where they are few (1 row of 2560 4.6 us, 64 of 5120 6.1, 600 of 4384 7.8).
+// read transposed.  Bound by the rows' reading where rows are many (4096 x 10576, rank 16: 24 us, 3.6 TB/s; 16384 x 2560, rank 32: 30 us,
+// 2.8 TB/s, the packing of the other factor included), by a unit's way through k where they are few (1 row of 2560 4.3 us, 64 of 5120 7.0, 600 of 4384 7.8).
 struct LowParams {
     const __bf16* x;
     int64_t ldx;

@@ -165,7 +165,7 @@ __device__ __forceinline__ float four_sums(const float (&a)[4]) {
 // scratch a lane, and a step of 96 heads, whose d_inner is 6144, took 8 % longer).  STEP: with the convolution step (fo.cs).  Template
 // arguments like MODE: a branch around loads ends in a wait for them.
 // LOW: a further wave works out the low-rank term of the workgroup's columns while the others stream w (one row 2560 -> 10576, rank 16:
-// 10.7 us, 5.1 TB/s, without a term 9.9).
+// 11.0 us, 4.9 TB/s, without a term 9.9).
 template <int MODE, int R, bool STEP, bool STREAM, bool LOW = false>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(FewParams fp, FewOperands fo, int cols) {
     extern __shared__ float few_sums[];  // [columns, whole fours][R][NW], then the squares [R][NW]

@@ -458,8 +458,8 @@ __global__ __launch_bounds__(GTHR, 1) void k_gemm_grads(GemmParams px, GemmParam
 }
 
 // A product with a low-rank term: the forward one (BK) or that of the input's gradient.  The term enters the accumulators while the first
-// K steps come in.  Bound by the matrix units like the plain product: 8192 rows 2560 -> 10576, rank 64, 358 us (1.24 PFLOP/s; without a
-// term 346); where tiles are fewer than compute units by those that have one: 1905 rows 5120 -> 2560, 160 tiles, rank 8, 63 us (without 63).
+// K steps come in.  Bound by the matrix units like the plain product: 8192 rows 2560 -> 10576, rank 64, 363 us (1.22 PFLOP/s; without a
+// term 346); where tiles are fewer than compute units by those that have one: 1905 rows 5120 -> 2560, 160 tiles, rank 8, 64 us (without 63).
 template <bool BK, int WJ>
 __global__ __launch_bounds__(GTHR, 1) void k_gemm_low(GemmParams gp, LowRankTerm lr) {
     gemm_tile<true, BK, WJ, true>(gp, blockIdx.x, &lr);
@@ -473,7 +473,7 @@ __global__ __launch_bounds__(GTHR, 1) void k_gemm_low_mixed(GemmParams p1, GemmP
 // 128 x 128 tiles for products whose 256-row tiles are too few (600 rows 1024 -> 4384 25 -> 21 us, 1000 rows 768 -> 3352 22 -> 18, narrow
 // product included; in more than one round the 256-row tiles are faster): eight waves of 64 x 64, each with half of a step's k (64 x 32 with
 // all of it reads half as much again from LDS: 2967 rows 1536 -> 768 19.2 us, 16.7 so), four buffers of a K step, loaded three steps
-// ahead, one barrier a step (the waves have left step t - 1: step t + 3 may come in where it was).  600 rows 1024 -> 4384, rank 8: 13.7 us.
+// ahead, one barrier a step (the waves have left step t - 1: step t + 3 may come in where it was).  600 rows 1024 -> 4384, rank 8: 14.8 us.
 template <bool BK>
 struct Half {
     typedef Tile<128, true> TA;
