@@ -439,13 +439,14 @@ def ssd_conv1d_bwd(u, w, bias, state_in, dout, dstate_out=None, want_dstate=True
     return {"du": du, "dw": dw, "dbias": dbias, "dstate_in": dstate_in}
 
 
-def _row_stride(t, name):
-    """Elements between the rows of t [rows, dim].  Rows that share memory (a broadcast row: distance 0, which the C ABI takes as dense) are
-    refused: the call would run over what the tensor does not have."""
-    rows, dim = t.shape
-    if rows > 1 and t.stride(0) < dim:
+def _row_stride(rows, dim, stride, name):
+    """Elements between the rows of a [rows, dim] tensor.  Rows that share memory (a broadcast row: distance 0, which the C ABI takes as dense)
+    are refused: the call would run over what the tensor does not have."""
+    if rows <= 1:
+        return dim
+    if stride < dim:
         raise ValueError(f"the rows of {name} must not share memory (a broadcast tensor needs .contiguous())")
-    return t.stride(0) if rows > 1 else dim
+    return stride
 
 
 def _norm_shape(y, z, ngroups, eps, *same_as):
@@ -461,7 +462,7 @@ def _norm_shape(y, z, ngroups, eps, *same_as):
     if dt == SSD_F32 and y.dtype != torch.float32:
         raise TypeError("dtype must be float32 or bfloat16")
     T, C = y.shape
-    return ssd_norm_shape_t(dt, C, ngroups, eps, T, _row_stride(y, "y"), C if z is None else _row_stride(z, "z"))
+    return ssd_norm_shape_t(dt, C, ngroups, eps, T, _row_stride(T, C, y.stride(0), "y"), C if z is None else _row_stride(T, C, z.stride(0), "z"))
 
 
 def _norm_weight(w, C):
@@ -511,9 +512,12 @@ def ssd_gated_norm_bwd(y, z, w, dout, eps=1e-5, ngroups=1, flags=0, dy=None, dz=
 
 def _rows_view(t, name):
     import torch
-    if t.dim() != 2 or not t.is_cuda or t.dtype != torch.bfloat16 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be a [rows, dim] bf16 device tensor with unit stride along dim")
-    return _row_stride(t, name)
+    if t.dim() == 2 and t.is_cuda and t.dtype == torch.bfloat16:
+        rows, dim = t.shape
+        stride, unit = t.stride()
+        if unit == 1 or dim <= 1:
+            return _row_stride(rows, dim, stride, name)
+    raise ValueError(f"{name} must be a [rows, dim] bf16 device tensor with unit stride along dim")
 
 
 def ssd_linear_fwd(x, w, out=None):
