@@ -369,7 +369,8 @@ int ssd_grad_clip(void* plan, int64_t pieces, const double* sum_sq, float max_no
  *             sequence checkpoints only the state entering a segment is kept (final_state of the segment before it), and the segment's
  *             states are what its forward call, run again, writes.
  *   workspace: ssd_gated_scan_workspace_bytes bytes, 256-byte aligned, contents undefined before and after; what is reported for a length
- *             does for every shorter one.  Calls that share it must not overlap in time (their results are then wrong or NaN).
+ *             does for every shorter one.  Calls that share it must not overlap in time: their results are then wrong or NaN, but they end, and
+ *             touch nothing beside the workspace and their own tensors.
  * ssd_gated_scan_step: the same for a few tokens of every sequence (seqlen, often 1), token by token, from state_in to state_out, which may be the
  * same memory.  No workspace; seq_reset must be NULL.
  * Arithmetic and states are fp32, each output is rounded once.  dtype fp32 or bf16, rate finite and positive, any C, L and alignment to whole

@@ -12,6 +12,7 @@
 #include <initializer_list>
 #include <type_traits>
 
+#include "chunk_places.h"
 #include "column_sums.h"
 
 namespace ssdk {
@@ -169,6 +170,7 @@ struct Chain {
     uint64_t* runs;     // [chunk][Bt][Cp]: A, H of a chunk
     uint32_t* ends;     // [group][Bt][Cp]: the state behind a group
     float* slopes;      // [Cp], of the channels that there are
+    uint32_t chunks;    // of a sequence
 };
 // Sets the words to "not there" and the counters to 0, and works out every channel's slope on the way: a launch's time, 2 us for 16 chunks of
 // 768 channels, 11 for 2048 of 2560.
@@ -191,13 +193,7 @@ struct Place {
 };
 template <bool CHAIN>
 __device__ __forceinline__ Place take_place(const ScanParams& sp, const Chain& ch, uint32_t* lds) {
-    // Workgroups go to the eight XCDs in turn.  Each takes tiles side by side, which share lines where rows are no whole number of them (8 x 22844
-    // tokens of 3672 channels, forward and backward: 3.80 ms, the tiles in turn as well 4.35; 30000 of 2561 506 us and 552), and goes on by
-    // as many from chunk to chunk: with the same ones for good it asks its L2 for an eighth of the lines' slots (65536 tokens of 5120 channels:
-    // 1.87 ms, going on 1.58).
-    const uint32_t tiles = (uint32_t)((sp.C + TILE - 1) / TILE), side = tiles * sp.Bt, each = side >> 3, rest = side & 7;
-    const uint32_t turn = blockIdx.x / side, pos = blockIdx.x - turn * side, xcd = pos & 7;
-    const uint32_t in = (xcd * each + (xcd < rest ? xcd : rest) + (pos >> 3) + turn * (each + 1)) % side;
+    const uint32_t tiles = (uint32_t)((sp.C + TILE - 1) / TILE), in = tile_of(blockIdx.x, tiles * sp.Bt);
     uint32_t chunk = 0;
     if (CHAIN) {
         if (threadIdx.x == 0) *lds = __hip_atomic_fetch_add(ch.tickets + in * TICKET, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -409,6 +405,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_gated_scan_fwd(ScanParams sp,
     __shared__ f32x4 totals[WAVES][2][16];  // the waves' runs
     __shared__ ChainLds L;
     const Place at = take_place<CHAIN>(sp, ch, &place);
+    if (CHAIN && !chunk_there((uint32_t)at.chunk, ch.chunks)) return;
     const Lane<K> me(at.c0, sp.C);
     const int64_t t0 = at.chunk * CHUNK, Cp = (int64_t)((sp.C + TILE - 1) / TILE) * TILE;
     const int rows = sp.L - t0 < CHUNK ? (int)(sp.L - t0) : CHUNK;
@@ -530,6 +527,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_gated_scan_bwd(ScanParams sp,
     __shared__ ChainLds L;
     __shared__ f32x4 later[2][K][64 * WAVES];  // each thread's own
     const Place at = take_place<CHAIN>(sp, ch, &place);
+    if (CHAIN && !chunk_there((uint32_t)at.chunk, ch.chunks)) return;
     const Lane<K> me(at.c0, sp.C);
     const int64_t chunk_at = sp.nchunks - 1 - at.chunk, t0 = chunk_at * CHUNK, Cp = (int64_t)((sp.C + TILE - 1) / TILE) * TILE;
     const int rows = sp.L - t0 < CHUNK ? (int)(sp.L - t0) : CHUNK;
@@ -825,7 +823,10 @@ Layout layout(const ScanParams& sp, bool bwd) {
     l.total = l.part + (bwd ? up256((size_t)(sp.nchunks > 0 ? sp.nchunks : 1) * sp.Bt * sp.C * 4) : 0);
     return l;
 }
-Chain chain_of(const Layout& l, void* ws) { return {(uint32_t*)((char*)ws + l.tickets), (uint64_t*)((char*)ws + l.runs), (uint32_t*)((char*)ws + l.ends), (float*)((char*)ws + l.slopes)}; }
+Chain chain_of(const Layout& l, void* ws) {
+    char* const p = (char*)ws;
+    return {(uint32_t*)(p + l.tickets), (uint64_t*)(p + l.runs), (uint32_t*)(p + l.ends), (float*)(p + l.slopes), (uint32_t)l.chunks};
+}
 // The launch in front, where there are several chunks.
 void clear_chain(const ScanParams& sp, const Layout& l, const Chain& ch, hipStream_t st) {
     if (l.chunks <= 1) return;
