@@ -373,8 +373,8 @@ int ssd_grad_clip(void* plan, int64_t pieces, const double* sum_sq, float max_no
  *             touch nothing beside the workspace and their own tensors.
  * ssd_gated_scan_step: the same for a few tokens of every sequence (seqlen, often 1), token by token, from state_in to state_out, which may be the
  * same memory.  No workspace; seq_reset must be NULL.
- * Arithmetic and states are fp32, each output is rounded once.  dtype fp32 or bf16, rate finite and positive, any C, L and alignment to whole
- * elements (vectors where C, strides and pointers are multiples of four elements); row strides up to 2^20 elements.  L == 0: final_state is init_state, dinit_state is
+ * Arithmetic and states are fp32, each output is rounded once.  dtype fp32 or bf16, rate finite and positive, C and row strides up to 2^20 elements, Bt
+ * up to 65535, L up to 2^32, and Bt ceil(C / 64) ceil(L / 64) below 2^31; alignment to whole elements.  L == 0: final_state is init_state, dinit_state is
  * dfinal_state, dlam zero.  Outputs must not overlap inputs or each other.  Everything is enqueued on hip_stream, nothing is allocated.
  * Errors: SSD_ERR_NULL, SSD_ERR_SHAPE, SSD_ERR_DTYPE, SSD_ERR_ARG, SSD_ERR_WORKSPACE, SSD_ERR_LAUNCH.
  */

@@ -18,4 +18,9 @@ constexpr uint32_t tile_of(uint32_t block, uint32_t side) {
 // its own it leaves alone, so that such calls stay inside their tensors.
 constexpr bool chunk_there(uint32_t drawn, uint32_t chunks) { return drawn < chunks; }
 
+// Workgroups of 256 threads that one launch takes: fewer than 2^32 threads.  More go out in launches one after another, workgroup `block` of the next being
+// number `first` + block of all; they go on with the counters, so that what a workgroup waits for still runs already or has run.
+constexpr uint32_t MOST_WORKGROUPS = (1u << 24) - 8;
+constexpr uint32_t workgroups_from(uint32_t first, uint32_t all) { return all - first < MOST_WORKGROUPS ? all - first : MOST_WORKGROUPS; }
+
 }  // namespace ssdk

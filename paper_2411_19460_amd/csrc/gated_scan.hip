@@ -70,6 +70,7 @@ struct ScanParams {
     int64_t x_rs, g_rs, o_rs, dx_rs, dg_rs, x_bs, g_bs, o_bs, dx_bs, dg_bs;
     int Bt, C;
     float rate;
+    uint32_t first;  // workgroups of the launches in front of this one
 };
 
 // ---- scan over chunks ----------------------------------------------------------------------------------------------------------------
@@ -89,6 +90,7 @@ struct ScanParams {
 constexpr int TILE = 64;    // channels of a workgroup
 constexpr int GROUP = 16;   // chunks
 constexpr int WAVES = 4, K_FWD = 8, K_BWD = 4;  // tokens of a chunk: 4 WAVES K
+static_assert(64 * WAVES * (uint64_t)MOST_WORKGROUPS < (uint64_t)1 << 32, "");
 static_assert(4 * WAVES * K_BWD == KEPT && K_FWD % K_BWD == 0 && GROUP % WAVES == 0, "");
 constexpr float CUT = -1.f;
 constexpr uint32_t NOT_THERE = 0xffffffffu;
@@ -193,7 +195,7 @@ struct Place {
 };
 template <bool CHAIN>
 __device__ __forceinline__ Place take_place(const ScanParams& sp, const Chain& ch, uint32_t* lds) {
-    const uint32_t tiles = (uint32_t)((sp.C + TILE - 1) / TILE), in = tile_of(blockIdx.x, tiles * sp.Bt);
+    const uint32_t tiles = (uint32_t)((sp.C + TILE - 1) / TILE), in = tile_of(sp.first + blockIdx.x, tiles * sp.Bt);
     uint32_t chunk = 0;
     if (CHAIN) {
         if (threadIdx.x == 0) *lds = __hip_atomic_fetch_add(ch.tickets + in * TICKET, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -791,7 +793,7 @@ int check(const ssd_gated_scan_shape_t* sh, ScanParams* sp) {
         if (sp->Bt > 1 && *bs[k] < least) return SSD_ERR_SHAPE;
         if (*bs[k] < 0 || *bs[k] > ((int64_t)1 << 46)) return SSD_ERR_SHAPE;
     }
-    // a launch has a workgroup for every chunk and tile
+    // a workgroup for every chunk and tile
     if (sp->nchunks * sp->Bt * ((sp->C + TILE - 1) / TILE) > 0x7fffffff) return SSD_ERR_SHAPE;
     return SSD_OK;
 }
@@ -854,11 +856,15 @@ bool fours(const ScanParams& sp, int dtype, bool bwd, std::initializer_list<cons
         else if (sp.reset) SCAN_LAUNCH3(KERNEL, T, false, true);      \
         else SCAN_LAUNCH3(KERNEL, T, false, false);                   \
     } while (0)
-#define SCAN_LAUNCH(KERNEL)                                                                                \
-    do {                                                                                                   \
-        const dim3 grid((unsigned)(lay.chunks * lay.side)), block(64 * WAVES);              \
-        if (sh->dtype == SSD_BF16) SCAN_LAUNCH2(KERNEL, bf16_t);                                           \
-        else SCAN_LAUNCH2(KERNEL, float);                                                                  \
+#define SCAN_LAUNCH(KERNEL)                                                                                    \
+    do {                                                                                                       \
+        const uint32_t all = (uint32_t)(lay.chunks * lay.side);                                                \
+        for (uint32_t now; sp.first < all; sp.first += now) {                                                  \
+            now = workgroups_from(sp.first, all);                                                              \
+            const dim3 grid(now), block(64 * WAVES);                                                           \
+            if (sh->dtype == SSD_BF16) SCAN_LAUNCH2(KERNEL, bf16_t);                                           \
+            else SCAN_LAUNCH2(KERNEL, float);                                                                  \
+        }                                                                                                      \
     } while (0)
 unsigned pass_grid(int64_t n) { return (unsigned)(n < 262144 ? (n + 255) / 256 : 1024); }
 int done() { return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH; }
@@ -928,6 +934,7 @@ extern "C" int ssd_gated_scan_bwd(const ssd_gated_scan_shape_t* sh, const void* 
     const bool vec = fours(sp, sh->dtype, true, {x, gate_r, gate_i, dout, dx, dgate_r, dgate_i});
     clear_chain(sp, lay, chain, st);
     SCAN_LAUNCH(k_gated_scan_bwd);
+    if (done() != SSD_OK) return SSD_ERR_LAUNCH;  // there are no shares to add up
     hipLaunchKernelGGL(k_gated_scan_dlam, dim3((sp.C + 63) / 64), dim3(COLSUM_THREADS), 0, st, sp.part, sp.nchunks * sp.Bt, sp.C, lam, dlam, accumulate);
     return done();
 }
