@@ -518,6 +518,7 @@ struct Row {
 };
 struct Elems {
     float t[8], du[8], v[8], fhat[8], shat[8], dout[8], post[8];
+    uint32_t keep;  // bit e: element e stays
 };
 template <typename TS, typename TF>
 __device__ __forceinline__ void join_elements(Elems& o, const JoinParams& jp, const Row& w, uint64_t seed, uint64_t offset, int64_t r, int c0) {
@@ -535,10 +536,10 @@ __device__ __forceinline__ void join_elements(Elems& o, const JoinParams& jp, co
     parameter<false>(pre, jp.pre_w, 0, dim, c0);
     parameter<false>(o.post, jp.post_w, 0, dim, c0);
     parameter<false>(gate, jp.gate, r / jp.gate_rows * dim, dim, c0);
-    const uint32_t keep = jp.drop.drop ? keep_bits(jp.drop, seed, offset, r * jp.groups + (c0 >> 3)) : 0xff;
+    o.keep = jp.drop.drop ? keep_bits(jp.drop, seed, offset, r * jp.groups + (c0 >> 3)) : 0xff;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const bool on = keep >> e & 1;
+        const bool on = o.keep >> e & 1;
         o.dout[e] = dout.get(e);
         o.shat[e] = s.get(e) * w.rstd_s;
         o.t[e] = ds.get(e) + w.rstd_s * (o.dout[e] * pre[e] - o.shat[e] * w.ms);
@@ -620,8 +621,8 @@ __global__ __launch_bounds__(64) void k_join_sums_wide(JoinParams jp) {
         if (jp.dalpha) x.fetch(jp.x, r * jp.s_rs, dim, c0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            // a dropped element adds nothing, whatever f holds
-            post[e] = o.du[e] == 0.f ? post[e] : fmaf(o.du[e], o.fhat[e], post[e]);
+            const bool on = o.keep >> e & 1;  // a dropped element adds nothing, whatever f holds
+            post[e] = on ? fmaf(o.du[e], o.fhat[e], post[e]) : post[e];
             pre[e] = fmaf(o.dout[e], o.shat[e], pre[e]);
             alpha[e] = fmaf(o.t[e], x.get(e), alpha[e]);
             gate[e] = fmaf(o.t[e], o.v[e], gate[e]);
