@@ -621,11 +621,11 @@ __global__ __launch_bounds__(64) void k_join_sums_wide(JoinParams jp) {
         if (jp.dalpha) x.fetch(jp.x, r * jp.s_rs, dim, c0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const bool on = o.keep >> e & 1;  // a dropped element adds nothing, whatever f holds
+            const bool on = o.keep >> e & 1;  // a dropped element adds nothing, whatever f, ds and dout hold
             post[e] = on ? fmaf(o.du[e], o.fhat[e], post[e]) : post[e];
             pre[e] = fmaf(o.dout[e], o.shat[e], pre[e]);
             alpha[e] = fmaf(o.t[e], x.get(e), alpha[e]);
-            gate[e] = fmaf(o.t[e], o.v[e], gate[e]);
+            gate[e] = on ? fmaf(o.t[e], o.v[e], gate[e]) : gate[e];
         }
         if (jp.dgate && (r + 1 == r1 || (r + 1) % jp.gate_rows == 0)) {
             const int64_t q = r / jp.gate_rows;

@@ -1,14 +1,57 @@
-"""The join's gradients where values are not finite, the same in rows that a workgroup holds in registers and in wider ones."""
+"""The join's gradients where values are not finite: a dropped element adds nothing to any sum, whatever it and its gradient hold; a kept one does, also where
+its gate is zero.  The same in rows that a workgroup holds in registers and in wider ones."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2411_19460_amd as pk
+from join_bounds import gradient_bounds
 from oracle import join_ref as ref
-from test_gpu_join import EPS, dev, draw, rng_of
+from test_gpu_join import EPS, TYPES, dev, draw, near, rng_of
 
 pytestmark = pytest.mark.gpu
 WIDTHS = [8200, 8196, 10243]
+
+
+def backward(d, dtype, stream, T, gate_rows, s, ds, p, f=None, x=True):
+    params = {k: dev(d[k]) for k in ("post_w", "gate", "alpha", "pre_w")}
+    return pk.ssd_join_bwd(s, dev(d["f"], dtype) if f is None else f, dev(d["dout"], dtype), ds=ds, x=dev(d["x"], stream) if x else None, **params,
+                           gate_rows=gate_rows, eps=EPS, p=p, rng=rng_of(1, 2))
+
+
+@pytest.mark.parametrize("dtype,stream", TYPES)
+@pytest.mark.parametrize("D", WIDTHS)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("post", [True, False])
+def test_a_gradient_of_a_dropped_element(dtype, stream, D, value, post):
+    """ds that is not finite where elements are dropped: dx has it there, and nothing else knows of it but dalpha's columns."""
+    T, p, gate_rows = 9, 0.3, 4
+    d = draw(D, dtype, stream, T, D, post=post, gate_rows=gate_rows)
+    keep = ref.mask(T, D, p, 1, 2)
+    places = [(r, int(np.argwhere(keep[r] == 0)[k, 0])) for r, k in ((0, 0), (3, -1), (4, 7), (8, 20)) if (keep[r] == 0).sum() > 20]
+    assert places
+    params = {k: dev(d[k]) for k in ("post_w", "gate", "alpha", "pre_w")}
+    s = pk.ssd_join_fwd(dev(d["x"], stream), dev(d["f"], dtype), **params, gate_rows=gate_rows, eps=EPS, p=p, rng=rng_of(1, 2))["s"]
+    ds = dev(d["ds"], stream)
+    for r, c in places:
+        ds[r, c] = value
+        d["ds"][r, c] = 0.0
+    q = backward(d, dtype, stream, T, gate_rows, s, ds, p)
+    sh = s.double().cpu().numpy()
+    gates = ref._gates(d["gate"], T, gate_rows)
+    g = ref.backward(sh, d["f"], d["dout"], d["ds"], d["x"], d["post_w"], d["gate"], gate_rows, d["alpha"], d["pre_w"], keep, EPS)
+    b = gradient_bounds(sh, d["f"], d["dout"], d["ds"], d["x"], d["post_w"], gates, d["alpha"], d["pre_w"], keep, EPS, g, T)
+    b["dgate"] = np.stack([b["dgate rows"][k:k + gate_rows].sum(0) for k in range(0, T, gate_rows)])
+    for name in ("df", "dgate", "dpre_w") + (("dpost_w",) if post else ()):
+        near(q[name], g[name], b[name], dtype if name == "df" else "f32", name)
+    rows, cols = (list(t) for t in zip(*places))
+    assert not bool(torch.isfinite(q["dx"][rows, cols]).any()) and not bool(torch.isfinite(q["dalpha"][cols]).any())
+    finite = torch.ones((T, D), dtype=torch.bool, device="cuda")
+    finite[rows, cols] = False
+    assert bool(torch.isfinite(q["dx"][finite]).all())
+    others = torch.ones(D, dtype=torch.bool, device="cuda")
+    others[cols] = False
+    assert bool(torch.isfinite(q["dalpha"][others]).all())
 
 
 @pytest.mark.parametrize("D", [264, *WIDTHS])
