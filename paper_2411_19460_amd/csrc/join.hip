@@ -401,7 +401,22 @@ __global__ __launch_bounds__(AHEAD ? 512 : 64 * MAX_WAVES, AHEAD && ALPHA ? 3 : 
         const float rstd_f = jp.post_w ? rsqrtf(s[0] * inv + jp.eps) : 1.f;
         const float rstd_s = jp.pre_w ? rsqrtf(s[1] * inv + jp.eps) : 0.f;
         const float ms = s[2] * inv * rstd_s;
-        const float mf = jp.post_w ? (s[3] + rstd_s * (s[4] - rstd_s * ms * s[5])) * inv * rstd_f : 0.f;
+        float mf = jp.post_w ? (s[3] + rstd_s * (s[4] - rstd_s * ms * s[5])) * inv * rstd_f : 0.f;
+        // Where ds or dout of a dropped element is not finite, k = 0 times that is no number, though nothing of it enters the mean: there the mean is taken of
+        // its own terms.  Every thread of the row has the same mf.
+        if (DROP && jp.post_w && !(fabsf(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, mf)))) < INFINITY)) {
+            float own_terms[6] = {};
+            fetch(post, POST);
+            fetch(pre, PRE);
+            fetch(gate, GATE);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float t = v.ds.get(e) + rstd_s * (v.dout.get(e) * pre[e] - v.s.get(e) * rstd_s * ms);
+                if (keep >> e & 1) own_terms[0] = fmaf(d.scale * gate[e] * t * post[e], v.f.get(e), own_terms[0]);
+            }
+            row_sums(L, own_terms, waves, side);
+            mf = own_terms[0] * inv * rstd_f;
+        }
         Eight<TS> dx;
         Eight<TF> df;
         fetch(post, POST);

@@ -11,6 +11,7 @@ from test_gpu_join import EPS, TYPES, dev, draw, near, rng_of
 
 pytestmark = pytest.mark.gpu
 WIDTHS = [8200, 8196, 10243]
+NARROW = [7, 8, 264, 512, 2560, 2561, 4104, 8191, 8192]
 
 
 def backward(d, dtype, stream, T, gate_rows, s, ds, p, f=None, x=True):
@@ -20,7 +21,7 @@ def backward(d, dtype, stream, T, gate_rows, s, ds, p, f=None, x=True):
 
 
 @pytest.mark.parametrize("dtype,stream", TYPES)
-@pytest.mark.parametrize("D", WIDTHS)
+@pytest.mark.parametrize("D", NARROW + WIDTHS)
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("post", [True, False])
 def test_a_gradient_of_a_dropped_element(dtype, stream, D, value, post):
@@ -28,7 +29,8 @@ def test_a_gradient_of_a_dropped_element(dtype, stream, D, value, post):
     T, p, gate_rows = 9, 0.3, 4
     d = draw(D, dtype, stream, T, D, post=post, gate_rows=gate_rows)
     keep = ref.mask(T, D, p, 1, 2)
-    places = [(r, int(np.argwhere(keep[r] == 0)[k, 0])) for r, k in ((0, 0), (3, -1), (4, 7), (8, 20)) if (keep[r] == 0).sum() > 20]
+    dropped = [np.argwhere(keep[r] == 0)[:, 0] for r in range(T)]
+    places = [(r, int(dropped[r][k % len(dropped[r])])) for r, k in ((0, 0), (3, -1), (4, 7), (8, 20)) if len(dropped[r])]
     assert places
     params = {k: dev(d[k]) for k in ("post_w", "gate", "alpha", "pre_w")}
     s = pk.ssd_join_fwd(dev(d["x"], stream), dev(d["f"], dtype), **params, gate_rows=gate_rows, eps=EPS, p=p, rng=rng_of(1, 2))["s"]
@@ -52,6 +54,19 @@ def test_a_gradient_of_a_dropped_element(dtype, stream, D, value, post):
     others = torch.ones(D, dtype=torch.bool, device="cuda")
     others[cols] = False
     assert bool(torch.isfinite(q["dalpha"][others]).all())
+
+
+@pytest.mark.parametrize("dtype,stream", TYPES)
+@pytest.mark.parametrize("D", [1, 5, *NARROW, *WIDTHS])
+@pytest.mark.parametrize("which", ["ds", "dout"])
+def test_where_everything_is_dropped(dtype, stream, D, which):
+    """Nothing of f enters the stream, so its gradient and those of its norm and gate are zero, whatever the gradients of the results."""
+    T = 5
+    d = draw(D, dtype, stream, T, D, gate_rows=2)
+    d[which][1, D // 2], d[which][4, 0] = np.inf, np.nan
+    q = backward(d, dtype, stream, T, 2, dev(d["x"], stream), dev(d["ds"], stream), 1.0)
+    for name in ("df", "dgate", "dpost_w"):
+        assert bool((q[name] == 0).all()), name
 
 
 @pytest.mark.parametrize("D", [264, *WIDTHS])
