@@ -18,9 +18,14 @@ constexpr uint32_t tile_of(uint32_t block, uint32_t side) {
 // its own it leaves alone, so that such calls stay inside their tensors.
 constexpr bool chunk_there(uint32_t drawn, uint32_t chunks) { return drawn < chunks; }
 
-// Workgroups of 256 threads that one launch takes: fewer than 2^32 threads.  More go out in launches one after another, workgroup `block` of the next being
-// number `first` + block of all; they go on with the counters, so that what a workgroup waits for still runs already or has run.
-constexpr uint32_t MOST_WORKGROUPS = (1u << 24) - 8;
-constexpr uint32_t workgroups_from(uint32_t first, uint32_t all) { return all - first < MOST_WORKGROUPS ? all - first : MOST_WORKGROUPS; }
+// A launch takes fewer than 2^32 threads, of 256 a workgroup, along a dimension.  More workgroups than that lie in rows of ROW, the last of them with
+// some to spare, which draw no chunk of the launch's.  Its number is a workgroup's place in the grid alone: an argument that says where a launch begins
+// is waited for in front of everything else (3 x 2001 tokens of 2048 channels, packed, forward and backward: 80.1 us, without 78.1).
+constexpr uint32_t ROW = 1u << 16, MOST_IN_LINE = (1u << 24) - 1;
+struct Grid {
+    uint32_t x, y;
+};
+constexpr Grid grid_of(uint32_t workgroups) { return workgroups <= MOST_IN_LINE ? Grid{workgroups, 1} : Grid{ROW, (workgroups - 1) / ROW + 1}; }
+constexpr uint32_t number_of(uint32_t x, uint32_t y) { return y * ROW + x; }
 
 }  // namespace ssdk

@@ -70,7 +70,6 @@ struct ScanParams {
     int64_t x_rs, g_rs, o_rs, dx_rs, dg_rs, x_bs, g_bs, o_bs, dx_bs, dg_bs;
     int Bt, C;
     float rate;
-    uint32_t first;  // workgroups of the launches in front of this one
 };
 
 // ---- scan over chunks ----------------------------------------------------------------------------------------------------------------
@@ -90,7 +89,7 @@ struct ScanParams {
 constexpr int TILE = 64;    // channels of a workgroup
 constexpr int GROUP = 16;   // chunks
 constexpr int WAVES = 4, K_FWD = 8, K_BWD = 4;  // tokens of a chunk: 4 WAVES K
-static_assert(64 * WAVES * (uint64_t)MOST_WORKGROUPS < (uint64_t)1 << 32, "");
+static_assert(64 * WAVES * (uint64_t)MOST_IN_LINE < (uint64_t)1 << 32, "");
 static_assert(4 * WAVES * K_BWD == KEPT && K_FWD % K_BWD == 0 && GROUP % WAVES == 0, "");
 constexpr float CUT = -1.f;
 constexpr uint32_t NOT_THERE = 0xffffffffu;
@@ -195,8 +194,8 @@ struct Place {
 };
 template <bool CHAIN>
 __device__ __forceinline__ Place take_place(const ScanParams& sp, const Chain& ch, uint32_t* lds) {
-    const uint32_t tiles = (uint32_t)((sp.C + TILE - 1) / TILE), in = tile_of(sp.first + blockIdx.x, tiles * sp.Bt);
-    uint32_t chunk = 0;
+    const uint32_t tiles = (uint32_t)((sp.C + TILE - 1) / TILE), side = tiles * sp.Bt, number = number_of(blockIdx.x, blockIdx.y), in = tile_of(number, side);
+    uint32_t chunk = number / side;
     if (CHAIN) {
         if (threadIdx.x == 0) *lds = __hip_atomic_fetch_add(ch.tickets + in * TICKET, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
@@ -407,7 +406,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_gated_scan_fwd(ScanParams sp,
     __shared__ f32x4 totals[WAVES][2][16];  // the waves' runs
     __shared__ ChainLds L;
     const Place at = take_place<CHAIN>(sp, ch, &place);
-    if (CHAIN && !chunk_there((uint32_t)at.chunk, ch.chunks)) return;
+    if (!chunk_there((uint32_t)at.chunk, CHAIN ? ch.chunks : 1)) return;
     const Lane<K> me(at.c0, sp.C);
     const int64_t t0 = at.chunk * CHUNK, Cp = (int64_t)((sp.C + TILE - 1) / TILE) * TILE;
     const int rows = sp.L - t0 < CHUNK ? (int)(sp.L - t0) : CHUNK;
@@ -529,7 +528,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_gated_scan_bwd(ScanParams sp,
     __shared__ ChainLds L;
     __shared__ f32x4 later[2][K][64 * WAVES];  // each thread's own
     const Place at = take_place<CHAIN>(sp, ch, &place);
-    if (CHAIN && !chunk_there((uint32_t)at.chunk, ch.chunks)) return;
+    if (!chunk_there((uint32_t)at.chunk, CHAIN ? ch.chunks : 1)) return;
     const Lane<K> me(at.c0, sp.C);
     const int64_t chunk_at = sp.nchunks - 1 - at.chunk, t0 = chunk_at * CHUNK, Cp = (int64_t)((sp.C + TILE - 1) / TILE) * TILE;
     const int rows = sp.L - t0 < CHUNK ? (int)(sp.L - t0) : CHUNK;
@@ -858,13 +857,10 @@ bool fours(const ScanParams& sp, int dtype, bool bwd, std::initializer_list<cons
     } while (0)
 #define SCAN_LAUNCH(KERNEL)                                                                                    \
     do {                                                                                                       \
-        const uint32_t all = (uint32_t)(lay.chunks * lay.side);                                                \
-        for (uint32_t now; sp.first < all; sp.first += now) {                                                  \
-            now = workgroups_from(sp.first, all);                                                              \
-            const dim3 grid(now), block(64 * WAVES);                                                           \
-            if (sh->dtype == SSD_BF16) SCAN_LAUNCH2(KERNEL, bf16_t);                                           \
-            else SCAN_LAUNCH2(KERNEL, float);                                                                  \
-        }                                                                                                      \
+        const Grid g = grid_of((uint32_t)(lay.chunks * lay.side));                                             \
+        const dim3 grid(g.x, g.y), block(64 * WAVES);                                                          \
+        if (sh->dtype == SSD_BF16) SCAN_LAUNCH2(KERNEL, bf16_t);                                               \
+        else SCAN_LAUNCH2(KERNEL, float);                                                                      \
     } while (0)
 unsigned pass_grid(int64_t n) { return (unsigned)(n < 262144 ? (n + 255) / 256 : 1024); }
 int done() { return hipGetLastError() == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH; }

@@ -1,4 +1,4 @@
-"""The longest calls that the gated recurrence takes, the first that it refuses, and the launches that a long one goes out in."""
+"""The longest calls that the gated recurrence takes, the first that it refuses, and the grid of a long one."""
 import ctypes
 import os
 import shutil
@@ -33,23 +33,23 @@ WALK = r"""
 #include "chunk_places.h"
 using namespace ssdk;
 int main() {
-    for (uint64_t all : {1ull, 300ull, (1ull << 24) - 9, (1ull << 24) - 8, (1ull << 24) - 7, 1ull << 24, 257ull * 65535, (1ull << 25) - 16, (1ull << 31) - 1}) {
-        uint64_t sum = 0;
-        uint32_t first = 0, launches = 0;
-        for (uint32_t now; first < (uint32_t)all; first += now, ++launches) {
-            now = workgroups_from(first, (uint32_t)all);
-            if (!now || now * 256ull >= 1ull << 32 || first % 8) return std::printf("%u workgroups from %u of %llu\n", now, first, (unsigned long long)all), 1;
-            sum += now;
-        }
-        if (sum != all || launches != (all + (1 << 24) - 9) / ((1 << 24) - 8)) return std::printf("%llu of %llu\n", (unsigned long long)sum, (unsigned long long)all), 1;
+    for (uint64_t all : {1ull, 300ull, (1ull << 24) - 2, (1ull << 24) - 1, 1ull << 24, (1ull << 24) + 1, 257ull * 65535, (1ull << 25) - 16, (1ull << 31) - 1}) {
+        const Grid g = grid_of((uint32_t)all);
+        const uint64_t there = (uint64_t)g.x * g.y;
+        bool good = there >= all && there - all < ROW && g.x * 256ull < 1ull << 32 && g.y < 65536 && there <= 1ull << 31;
+        good = good && (g.y > 1 || there == all);
+        // rows follow one another, and whole turns of the eight XCDs make a row
+        for (uint32_t y = 1; y < g.y; ++y) good = good && number_of(0, y) == number_of(g.x - 1, y - 1) + 1 && number_of(0, y) % 8 == 0;
+        good = good && number_of(0, 0) == 0 && number_of(g.x - 1, g.y - 1) == there - 1;
+        if (!good) return std::printf("%u x %u workgroups for %llu\n", g.x, g.y, (unsigned long long)all), 1;
     }
     return 0;
 }
 """
 
 
-def test_launches_of_a_long_call(tmp_path):
-    """Each carries less than 2^32 threads, and together they have every workgroup once."""
+def test_the_grid_of_a_long_call(tmp_path):
+    """Every workgroup once, in order, less than 2^32 threads along a dimension, and less than a row to spare."""
     cxx = shutil.which("g++") or shutil.which("c++")
     if cxx is None:
         pytest.skip("no host compiler")
