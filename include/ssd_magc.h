@@ -356,7 +356,8 @@ int ssd_grad_clip(void* plan, int64_t pieces, const double* sum_sq, float max_no
  *     a = exp(-rate softplus(lam[c]) r)                                the decay, between 0 and 1
  *     h_t = a h_{t-1} + sqrt(1 - a^2) i x[b,t,c]                       out[b,t,c] = h_t
  * A token whose seq_reset flag is non-zero starts a new sequence: h_{t-1} is taken as zero there, in out and in every gradient, and nothing of
- * the tokens before is read for it (an infinity or a NaN stays in its sequence).
+ * the tokens before is read for it (an infinity or a NaN stays in its sequence; what comes behind it there is infinite or NaN).  Every token's input is scaled by
+ * sqrt(1 - a^2), the first one's too.
  *   x         [Bt,L,C] dtype, rows x_row_stride elements apart, batches x_batch_stride
  *   gate_r, gate_i    likewise with gate_row_stride, gate_batch_stride: all three may be column slices of one projection's output
  *   dx, dgate_r, dgate_i    likewise with dx_row_stride, dx_batch_stride, dgate_row_stride, dgate_batch_stride
@@ -437,7 +438,8 @@ int ssd_dropout(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_t
  * wanted); one without its parameter is refused.  dx may be ds, df may be f, and s may be x in the forward call, with the same strides; else nothing may overlap.
  *   workspace: ssd_join_workspace_bytes bytes, 256-byte aligned (backward only: partial sums).  What is reported for a number of rows
  *              does for every smaller one.
- * Sums run in a fixed order.  Everything is enqueued on hip_stream, nothing is allocated.
+ * Sums are fp32 and run in a fixed order.  A dropped element adds nothing to df, dgate and dpost_w, whatever f and its gradient hold (an infinity or a NaN in ds too).
+ * Everything is enqueued on hip_stream, nothing is allocated.
  * Errors: SSD_ERR_NULL, SSD_ERR_SHAPE, SSD_ERR_DTYPE, SSD_ERR_ARG, SSD_ERR_WORKSPACE, SSD_ERR_LAUNCH.
  */
 typedef struct ssd_join_shape_t {

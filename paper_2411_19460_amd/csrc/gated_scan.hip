@@ -34,7 +34,7 @@ __device__ __forceinline__ Sig sigmoid2(float z) {
 __device__ __forceinline__ float sigmoid1(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -LOG2E)); }
 
 // From log2(a) = l2 <= 0: a, m = sqrt(1 - a^2) and 1 / m.  1 - a^2 = 1 - e^w with w = 2 ln a loses its leading digits near a = 1: above
-// w = -1/4 it is -w times a polynomial for (e^w - 1) / w, interpolated at the five Chebyshev points of [-1/4, 0] (off by 5e-9 of itself).
+// w = -1/4 it is -w times a polynomial for (e^w - 1) / w, interpolated at the five Chebyshev points of [-1/4, 0] (off by 7.3e-9 of itself, its coefficients in fp32).
 // m is 0 where 1 - a^2 is, and 1 / m is then held at a finite value: what it is multiplied by is 0 too.
 struct Decay {
     float a, m, rm;
@@ -173,8 +173,8 @@ struct Chain {
     float* slopes;      // [Cp], of the channels that there are
     uint32_t chunks;    // of a sequence
 };
-// Sets the words to "not there" and the counters to 0, and works out every channel's slope on the way: a launch's time, 2 us for 16 chunks of
-// 768 channels, 11 for 2048 of 2560.
+// Sets the words to "not there" and the counters to 0, and works out every channel's slope on the way: a launch's time, 2.3 us for 16 chunks of
+// 768 channels, 12 for 2048 of 2560.
 __global__ __launch_bounds__(256) void k_gated_scan_clear(Chain ch, int64_t side, uint4* words, int64_t n, const float* lam, int C, float rate) {
     const int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)gridDim.x * 256;
     for (int64_t i = i0; i < side; i += all) ch.tickets[i * TICKET] = 0;
@@ -195,7 +195,7 @@ struct Place {
 template <bool CHAIN>
 __device__ __forceinline__ Place take_place(const ScanParams& sp, const Chain& ch, uint32_t* lds) {
     const uint32_t tiles = (uint32_t)((sp.C + TILE - 1) / TILE), side = tiles * sp.Bt, number = number_of(blockIdx.x, blockIdx.y), in = tile_of(number, side);
-    uint32_t chunk = number / side;
+    uint32_t chunk = number / side;  // where there is one chunk: 0, or a workgroup to spare
     if (CHAIN) {
         if (threadIdx.x == 0) *lds = __hip_atomic_fetch_add(ch.tickets + in * TICKET, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
@@ -397,8 +397,8 @@ __device__ __forceinline__ void either(bool begins, Work work) {
     else work(std::false_type());
 }
 
-// Forward.  Bound by memory and vector units alike (39 instructions a value): 262144 tokens of 2560 channels, bf16, 1030 us (5.4 GB, 5.2 TB/s), fp32 1999
-// of 768 8.4; 3 x 2001 of 2048 30: two rounds of workgroups, the second half filled.  Four tokens a thread instead of eight double the chain: slower.
+// Forward.  Bound by memory and vector units alike (39 instructions a value): 262144 tokens of 2560 channels, bf16, 989 us (5.4 GB, 5.4 TB/s), fp32 1999
+// of 768 8.3; 3 x 2001 of 2048 31: two rounds of workgroups, the second half filled.  Four tokens a thread instead of eight double the chain: slower.
 template <typename T, bool VEC, bool RESET, bool CHAIN>
 __global__ __launch_bounds__(64 * WAVES, 4) void k_gated_scan_fwd(ScanParams sp, Chain ch) {
     constexpr int K = K_FWD, CHUNK = 4 * WAVES * K;
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_gated_scan_fwd(ScanParams sp,
 
 // Backward, chunks from the last to the first.  The states inside the chunk are worked out again from the one that the forward call kept, which
 // needs nothing of other chunks; the adjoint is a recurrence of the same form from behind, e_t = a_t (dout_t + e_{t+1}).  Three workgroups a compute unit (168
-// registers; four spill and are slower).  262144 tokens of 2560 channels, bf16: 2160 us (9.4 GB, 4.3 TB/s; 74 instructions a value), 3 x 2001 of 2048 44.
+// registers; four spill and are slower).  262144 tokens of 2560 channels, bf16: 2047 us (9.4 GB, 4.6 TB/s; 74 instructions a value), 3 x 2001 of 2048 46.
 template <typename T, bool VEC, bool RESET, bool CHAIN>
 __global__ __launch_bounds__(64 * WAVES, 3) void k_gated_scan_bwd(ScanParams sp, Chain ch) {
     constexpr int K = K_BWD, CHUNK = 4 * WAVES * K;
@@ -698,7 +698,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_gated_scan_bwd(ScanParams sp,
 }
 
 // dlam = sigmoid(lam) / softplus(lam) times the sum of the chunks' sums, in fp64 (there may be thousands) and in a fixed order.  4096 chunks of 2560
-// channels 28 us, 96 of 2048 4.5.
+// channels 28 us, 96 of 2048 4.7.
 __global__ __launch_bounds__(COLSUM_THREADS) void k_gated_scan_dlam(const float* part, int64_t nparts, int C, const float* lam, float* dlam, int accumulate) {
     __shared__ double red[COLSUM_WAVES][64];
     constexpr int U = 8;
@@ -727,7 +727,7 @@ __global__ __launch_bounds__(COLSUM_THREADS) void k_gated_scan_dlam(const float*
 }
 
 // A few tokens: four channels of a sequence a thread, token after token, the next token's inputs under way.  Bound by latency: one token of 2560 channels
-// 4.3 us, of 64 x 5120 5.2.
+// 4.2 us, of 64 x 5120 5.2.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(64) void k_gated_scan_step(ScanParams sp) {
     const int c = (blockIdx.x * 64 + threadIdx.x) * 4, b = blockIdx.y, left = sp.C - c;

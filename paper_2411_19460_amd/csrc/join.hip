@@ -225,7 +225,7 @@ __device__ __forceinline__ uint32_t keep_bits(const DropJob& d, uint64_t seed, u
 // Rows of up to ROW_DIM values: as many waves as it takes hold a row, eight values a thread, and walk the rows of a part one after
 // another, the next one under way while this one is worked on.  No branch hides a store, so that a row's wait
 // is for its loads and not for the stores behind them (with branches around them 300 us).  Parameters stay in registers (the gate until it
-// changes).  65536 rows of 2560, bf16, dropout: 258 us (1.34 GB, 5.2 TB/s).
+// changes).  65536 rows of 2560, bf16, dropout: 224 us (1.34 GB, 6.0 TB/s).
 template <typename TS, typename TF, bool VEC, bool DROP, bool, bool>  // the last two are the backward kernel's
 __global__ __launch_bounds__(64 * MAX_WAVES) void k_join_fwd(JoinParams jp) {
     __shared__ RowLds<1> L;
@@ -296,8 +296,8 @@ __global__ __launch_bounds__(64 * MAX_WAVES) void k_join_fwd(JoinParams jp) {
 // exchange between the waves does: with k = mask gate post_w f rstd_f (rstd_f taken out of the sum)
 //     sum k t = sum k ds + rstd_s sum k dout pre_w - rstd_s^2 ms sum k s
 // Parameters lie in LDS, each thread's own, since registers decide how many rows a compute unit has under way: three workgroups of five
-// waves (128 registers).  AHEAD: the next row comes in while this one is worked on.  65536 rows of 2560, bf16, dropout, three parameters: 486 us
-// (2.0 GB, 4.1 TB/s; without AHEAD 509; two workgroups of 146 registers, AHEAD, 676).
+// waves (128 registers).  AHEAD: the next row comes in while this one is worked on.  65536 rows of 2560, bf16, dropout, three parameters: 453 us
+// (2.0 GB, 4.4 TB/s).  When it was chosen, on another card: 486, without AHEAD 509; two workgroups of 146 registers, AHEAD, 676.
 template <typename TS, typename TF, bool VEC, bool DROP, bool ALPHA, bool AHEAD>
 __global__ __launch_bounds__(AHEAD ? 512 : 64 * MAX_WAVES, AHEAD && ALPHA ? 3 : 4) void k_join_bwd(JoinParams jp) {
     __shared__ RowLds<6> L;
@@ -474,7 +474,7 @@ __global__ __launch_bounds__(AHEAD ? 512 : 64 * MAX_WAVES, AHEAD && ALPHA ? 3 : 
 }
 
 // Rows wider than that: a workgroup a row, eights in turn, the row read again for every sum that needs the one before (20000 rows of 10240,
-// bf16, forward and backward: 1970 us, 2.3 TB/s of what has to be moved; element by element 6344).
+// bf16, forward and backward: 1695 us, 2.4 TB/s of what has to be moved; with a residual scale, on another card, 1970, element by element 6344).
 template <typename TS, typename TF>
 __global__ __launch_bounds__(256) void k_join_fwd_wide(JoinParams jp) {
     __shared__ float lds[4];
@@ -713,7 +713,7 @@ __global__ __launch_bounds__(COLSUM_THREADS) void k_join_reduce(JoinParams jp, i
     if (threadIdx.x < 64 && live) to[c] = jp.accumulate ? to[c] + s : s;
 }
 
-// Dropout alone, a call of the generator and eight values a thread, bound by memory (65536 rows of 5120, bf16: 1.34 GB, 259 us, 5.2 TB/s; an element a
+// Dropout alone, a call of the generator and eight values a thread, bound by memory (65536 rows of 5120, bf16: 1.34 GB, 251 us, 5.3 TB/s; an element a
 // thread 931).  A workgroup takes 256 consecutive eights; where the first of them lies is worked out once for all.  VEC: rows of whole eights on
 // 16 bytes, for bf16 alone: 30000 rows of 2560 forward and backward 125 us, without 131; fp32 232, without 221.
 template <typename T, bool VEC>
