@@ -438,7 +438,8 @@ int ssd_dropout(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_t
  * wanted); one without its parameter is refused.  dx may be ds, df may be f, and s may be x in the forward call, with the same strides; else nothing may overlap.
  *   workspace: ssd_join_workspace_bytes bytes, 256-byte aligned (backward only: partial sums).  What is reported for a number of rows
  *              does for every smaller one.
- * Sums are fp32 and run in a fixed order.  A dropped element adds nothing to df, dgate and dpost_w, whatever f and its gradient hold (an infinity or a NaN in ds too).
+ * Sums are fp32 and run in a fixed order.  A dropped element adds nothing to df, dgate and dpost_w, whatever its gradient is (an infinity or a NaN too);
+ * of f's own values the norm with post_w takes dropped ones too.
  * Everything is enqueued on hip_stream, nothing is allocated.
  * Errors: SSD_ERR_NULL, SSD_ERR_SHAPE, SSD_ERR_DTYPE, SSD_ERR_ARG, SSD_ERR_WORKSPACE, SSD_ERR_LAUNCH.
  */
